@@ -29,7 +29,7 @@
  * buffer it passes and keeps it alive until som_sync (or a synchronising call) returns; the library owns only
  * its internal workspaces.  A context is bound to one device and is not thread-safe.
  *
- * Calls that only enqueue (som_bmu, som_accumulate, som_neighborhood_update, som_topology, som_epoch without stats) may be
+ * Calls that only enqueue (som_bmu, som_accumulate, som_neighborhood_update, som_topology, som_epoch without stats, the local models' calls) may be
  * recorded into a HIP graph once the context has served the same call outside of one, and the graph replayed in stream
  * order with other calls on the context: workspaces are allocated on demand, which capture forbids, and a later call that
  * needs a larger one frees what the graph still uses.
@@ -312,6 +312,84 @@ int som_epoch_host(som_ctx* ctx, const float* Xhost, int64_t N, int32_t D, int64
 int som_epoch_file(som_ctx* ctx, int fd, int64_t offset, int64_t N, int32_t D, int64_t chunk_rows,
                    float* W, int32_t K, const float* G, double sigma, int kernel, double eps_h,
                    som_stats* stats);
+
+/*
+ * Local models: one matrix per node.  A map (or any router) names one or more nodes for every row; the rows are sorted by node,
+ * each goes through its node's matrix, and a row's results are added up again with its weights.  Rows and matrices are
+ * float32, bfloat16 or float16 (`type`); sums are float32 whatever the type, and a result is rounded once when it is stored.
+ * Every result has one order of summation: two calls on equal inputs give equal bits, whatever som_set_reproducible says.
+ *
+ * T rows with k nodes each are the pairs p = t k + j.  Pairs whose node lies outside [0, K) (padding, a row that found no place)
+ * have no place, contribute nothing and get nothing.  M is the number of places a sorted matrix holds (T k, or more); places from
+ * offsets[K] on belong to no node, and what calls would write there is left as it was.  Entries of slot and offsets that point outside
+ * M are not followed.  Matrices have leading dimensions of their own (>= their width, <= 2^21), any alignment of their elements serves;
+ * widths are at most 2^20, T k and M at most 2^31 - 1, K at most 32768.  Outputs must not overlap inputs or one another.
+ */
+enum { SOM_ROWS_FLOAT = 0 /* float32 */, SOM_ROWS_BFLOAT = 1 /* bfloat16 */, SOM_ROWS_HALF = 2 /* float16 */ };
+
+/*
+ * Places of the pairs in the nodes' order, pairs of a node in the order of p (a stable sort).
+ *   node [device] int32[T*k]: nodes of the rows, such as som_bmu's bmu for k = 1
+ *   offsets [device] int32[K+1]: node e's pairs have places offsets[e] .. offsets[e+1]-1; offsets[K] pairs have a node
+ *   order [device] int32[T*k] or NULL: the pair at each place, -1 from offsets[K] on
+ *   slot [device] int32[T*k] or NULL: the place of each pair, -1 without a node
+ * T = 0 is allowed (offsets becomes zeros).
+ */
+int som_group(som_ctx* ctx, const int32_t* node, int64_t T, int32_t k, int32_t K, int32_t* offsets, int32_t* order, int32_t* slot);
+
+/*
+ * Rows to their places: Y[slot[t*k+j]] = w_tj X[t].
+ *   X [device] T x D, ldx;  slot [device] int32[T*k];  weight [device] float[T*k] or NULL (w = 1: plain copies)
+ *   Y [device] M x D, ldy
+ * Its gradient: som_combine with the same weights takes dY to dX, and som_combine_grad with X as dout gives dweight.
+ */
+int som_dispatch(som_ctx* ctx, int type, const void* X, int64_t T, int32_t D, int64_t ldx, const int32_t* slot, int32_t k, const float* weight,
+                 void* Y, int64_t M, int64_t ldy);
+
+/*
+ * Rows back: out[t] = sum_j w_tj Y[slot[t*k+j]], j ascending; a row without places becomes zeros.
+ *   Y [device] M x D, ldy;  slot, weight as above;  out [device] T x D, ldo
+ */
+int som_combine(som_ctx* ctx, int type, const void* Y, int64_t M, int32_t D, int64_t ldy, const int32_t* slot, int64_t T, int32_t k,
+                const float* weight, void* out, int64_t ldo);
+
+/*
+ * Gradient of som_combine: dY[slot[t*k+j]] = w_tj dout[t],  dweight[t*k+j] = <dout[t], Y[slot[t*k+j]]> (0 without a place).
+ *   dY [device] M x D, lddy, or NULL;  dweight [device] float[T*k] or NULL (Y is not read then);  one of them at least
+ */
+int som_combine_grad(som_ctx* ctx, int type, const void* dout, int64_t T, int32_t D, int64_t lddo, const void* Y, int64_t M, int64_t ldy,
+                     const int32_t* slot, int32_t k, const float* weight, void* dY, int64_t lddy, float* dweight);
+
+enum {
+    SOM_ACT_NONE = 0,
+    SOM_ACT_RELU = 1,
+    SOM_ACT_SILU = 2,     /* z / (1 + exp(-z)) */
+    SOM_ACT_GELU = 3,     /* z (1 + erf(z / sqrt 2)) / 2 */
+    SOM_ACT_GELU_TANH = 4 /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 */
+};
+
+/*
+ * Rows times their node's matrix, with bias, activation and residual:  z_s = A_e x_s + c_e,  Y_s = act(z_s) + residual_s
+ * for the places s = offsets[e] .. offsets[e+1]-1 of node e.
+ *   X [device] M x Din, ldx;  offsets [device] int32[K+1], not decreasing, or NULL: K = 1 and all M rows are that node's
+ *   A [device] K x Dout x Din, dense;  bias [device] K x Dout, dense, or NULL;  residual [device] M x Dout, ldr, or NULL
+ *   pre [device] M x Dout, ldpre, or NULL: receives z, which the gradient of an activation needs
+ *   Y [device] M x Dout, ldy
+ */
+int som_node_product(som_ctx* ctx, int type, const void* X, int64_t M, int32_t Din, int64_t ldx, const int32_t* offsets, int32_t K, const void* A,
+                     int32_t Dout, const void* bias, int activation, const void* residual, int64_t ldr, void* pre, int64_t ldpre, void* Y, int64_t ldy);
+
+/*
+ * Its gradient: dz_s = dY_s act'(z_s);  dX_s = A_e^T dz_s,  dA_e = sum_s dz_s x_s^T,  dbias_e = sum_s dz_s  (a node without rows:
+ * zeros); the residual's gradient is dY.  dz is rounded to `type` (the matrix pipe's operand) where an activation changes it.
+ *   dY [device] M x Dout, lddy;  X, offsets, A as above (A is read for dX, X for dA);  pre [device] as som_node_product wrote it,
+ *   required unless activation is SOM_ACT_NONE
+ *   dX [device] M x Din, lddx, or NULL;  dA [device] K x Dout x Din, dense, or NULL;  dbias [device] K x Dout, dense, or NULL;
+ *   one of them at least
+ */
+int som_node_product_grad(som_ctx* ctx, int type, const void* dY, int64_t M, int32_t Dout, int64_t lddy, const void* X, int32_t Din, int64_t ldx,
+                          const int32_t* offsets, int32_t K, const void* A, const void* pre, int64_t ldpre, int activation, void* dX, int64_t lddx,
+                          void* dA, void* dbias);
 
 #ifdef __cplusplus
 }

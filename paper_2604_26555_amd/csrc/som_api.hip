@@ -64,6 +64,14 @@ static int grow(som_ctx* ctx, T** p, size_t* have, size_t want, const char* what
     return SOM_OK;
 }
 
+int models_workspace(som_ctx* ctx, size_t bytes)
+{
+    char* p = (char*)ctx->models_blob;
+    const int rc = grow(ctx, &p, &ctx->models_bytes, bytes, "the local models' workspace");
+    ctx->models_blob = p;
+    return rc;
+}
+
 static int common_checks(som_ctx* ctx, const void* X, int64_t N, int32_t D, int64_t ldx, const uint32_t* idx, int64_t m,
                          const void* W, int32_t K)
 {
@@ -166,6 +174,7 @@ void som_destroy(som_ctx* c)
     if (c->upd_blob) (void)hipFree(c->upd_blob);
     if (c->small_sums) (void)hipFree(c->small_sums);
     if (c->topo_blob) (void)hipFree(c->topo_blob);
+    if (c->models_blob) (void)hipFree(c->models_blob);
     if (c->S) (void)hipFree(c->S);
     if (c->n) (void)hipFree(c->n);
     if (c->qe) (void)hipFree(c->qe);
@@ -322,6 +331,146 @@ int som_neighborhood_update_static(som_ctx* ctx, const double* S, const uint64_t
         return check_hip(ctx, hipMemcpyAsync(n_guarded, ctx->small, sizeof(int32_t), hipMemcpyDeviceToDevice, ctx->stream),
                          "copying the guarded-node count");
     return SOM_OK;
+}
+
+// Rows of the local models: element type, sizes, and leading dimension of a matrix that holds values.
+static int rows_checks(som_ctx* ctx, int type, int64_t rows, int32_t D, const char* what)
+{
+    if (type != SOM_ROWS_FLOAT && type != SOM_ROWS_BFLOAT && type != SOM_ROWS_HALF) return fail(ctx, SOM_EINVAL, "unknown element type %d", type);
+    if (rows < 0) return fail(ctx, SOM_EINVAL, "%s: negative number of rows", what);
+    if (rows > 0x7fffffffLL) return fail(ctx, SOM_EINVAL, "%s: more than 2^31-1 rows per call", what);
+    if (D < 1 || D > kModelWidth) return fail(ctx, SOM_EINVAL, "%s: width %d outside 1..%d", what, D, kModelWidth);
+    return SOM_OK;
+}
+
+static int matrix_check(som_ctx* ctx, const void* p, int64_t rows, int32_t D, int64_t ld, int type, bool required, const char* what)
+{
+    if (rows == 0) return SOM_OK;
+    if (!p) return required ? fail(ctx, SOM_EINVAL, "null %s", what) : SOM_OK;
+    if (ld < D) return fail(ctx, SOM_EINVAL, "%s: leading dimension (%lld) is smaller than the width (%d)", what, (long long)ld, D);
+    if (ld > kModelStride) return fail(ctx, SOM_EINVAL, "%s: leading dimension (%lld) above %d", what, (long long)ld, kModelStride);
+    if ((uintptr_t)p % (type == SOM_ROWS_FLOAT ? 4 : 2)) return fail(ctx, SOM_EINVAL, "%s is not aligned to its elements", what);
+    if (!device_readable(p)) return fail(ctx, SOM_EINVAL, "%s must be device-accessible memory", what);
+    return SOM_OK;
+}
+
+static int array_check(som_ctx* ctx, const void* p, int64_t count, bool required, const char* what)
+{
+    if (count == 0) return SOM_OK;
+    if (!p) return required ? fail(ctx, SOM_EINVAL, "null %s", what) : SOM_OK;
+    if ((uintptr_t)p % 4) return fail(ctx, SOM_EINVAL, "%s is not aligned to 4 bytes", what);
+    return device_readable(p) ? SOM_OK : fail(ctx, SOM_EINVAL, "%s must be device-accessible memory", what);
+}
+
+static int pairs_check(som_ctx* ctx, int64_t rows, int32_t k)
+{
+    if (rows < 0) return fail(ctx, SOM_EINVAL, "negative number of rows");
+    if (k < 1) return fail(ctx, SOM_EINVAL, "a row needs one node at least (k=%d)", k);
+    if (rows > 0x7fffffffLL / k) return fail(ctx, SOM_EINVAL, "more than 2^31-1 pairs of row and node per call");
+    return SOM_OK;
+}
+
+int som_group(som_ctx* ctx, const int32_t* node, int64_t T, int32_t k, int32_t K, int32_t* offsets, int32_t* order, int32_t* slot)
+{
+    if (!ctx) return SOM_EINVAL;
+    if (int rc = pairs_check(ctx, T, k)) return rc;
+    if (K < 1 || K > kGroupNodes) return fail(ctx, SOM_EINVAL, "K (%d) outside 1..%d", K, kGroupNodes);
+    if (int rc = array_check(ctx, node, T, true, "node")) return rc;
+    if (int rc = array_check(ctx, offsets, 1, true, "offsets")) return rc;
+    if (int rc = array_check(ctx, order, T, false, "order")) return rc;
+    if (int rc = array_check(ctx, slot, T, false, "slot")) return rc;
+    if (int rc = check_hip(ctx, hipSetDevice(ctx->device), "hipSetDevice")) return rc;
+    return group_run(ctx, node, T * k, K, offsets, order, slot);
+}
+
+int som_dispatch(som_ctx* ctx, int type, const void* X, int64_t T, int32_t D, int64_t ldx, const int32_t* slot, int32_t k, const float* weight,
+                 void* Y, int64_t M, int64_t ldy)
+{
+    if (!ctx) return SOM_EINVAL;
+    if (int rc = pairs_check(ctx, T, k)) return rc;
+    if (int rc = rows_checks(ctx, type, M, D, "Y")) return rc;
+    if (int rc = matrix_check(ctx, X, T, D, ldx, type, true, "X")) return rc;
+    if (int rc = matrix_check(ctx, Y, T ? M : 0, D, ldy, type, true, "Y")) return rc;
+    if (int rc = array_check(ctx, slot, T, true, "slot")) return rc;
+    if (int rc = array_check(ctx, weight, T, false, "weight")) return rc;
+    if (int rc = check_hip(ctx, hipSetDevice(ctx->device), "hipSetDevice")) return rc;
+    return dispatch_run(ctx, type, X, T, D, ldx, slot, k, weight, Y, M, ldy);
+}
+
+int som_combine(som_ctx* ctx, int type, const void* Y, int64_t M, int32_t D, int64_t ldy, const int32_t* slot, int64_t T, int32_t k,
+                const float* weight, void* out, int64_t ldo)
+{
+    if (!ctx) return SOM_EINVAL;
+    if (int rc = pairs_check(ctx, T, k)) return rc;
+    if (int rc = rows_checks(ctx, type, M, D, "Y")) return rc;
+    if (int rc = matrix_check(ctx, Y, T ? M : 0, D, ldy, type, true, "Y")) return rc;
+    if (int rc = matrix_check(ctx, out, T, D, ldo, type, true, "out")) return rc;
+    if (int rc = array_check(ctx, slot, T, true, "slot")) return rc;
+    if (int rc = array_check(ctx, weight, T, false, "weight")) return rc;
+    if (int rc = check_hip(ctx, hipSetDevice(ctx->device), "hipSetDevice")) return rc;
+    return combine_run(ctx, type, Y, M, D, ldy, slot, T, k, weight, out, ldo);
+}
+
+int som_combine_grad(som_ctx* ctx, int type, const void* dout, int64_t T, int32_t D, int64_t lddo, const void* Y, int64_t M, int64_t ldy,
+                     const int32_t* slot, int32_t k, const float* weight, void* dY, int64_t lddy, float* dweight)
+{
+    if (!ctx) return SOM_EINVAL;
+    if (int rc = pairs_check(ctx, T, k)) return rc;
+    if (int rc = rows_checks(ctx, type, M, D, "Y")) return rc;
+    if (!dY && !dweight) return fail(ctx, SOM_EINVAL, "neither dY nor dweight is asked for");
+    if (int rc = matrix_check(ctx, dout, T, D, lddo, type, true, "dout")) return rc;
+    if (int rc = matrix_check(ctx, Y, T && dweight ? M : 0, D, ldy, type, true, "Y")) return rc;
+    if (int rc = matrix_check(ctx, dY, T ? M : 0, D, lddy, type, false, "dY")) return rc;
+    if (int rc = array_check(ctx, slot, T, true, "slot")) return rc;
+    if (int rc = array_check(ctx, weight, T, false, "weight")) return rc;
+    if (int rc = array_check(ctx, dweight, T, false, "dweight")) return rc;
+    if (int rc = check_hip(ctx, hipSetDevice(ctx->device), "hipSetDevice")) return rc;
+    return combine_grad_run(ctx, type, dout, T, D, lddo, Y, M, ldy, slot, k, weight, dY, lddy, dweight);
+}
+
+static int models_checks(som_ctx* ctx, int type, int64_t M, int32_t Din, int32_t Dout, const int32_t* offsets, int32_t K, const void* A, bool needs_A,
+                         int activation)
+{
+    if (int rc = rows_checks(ctx, type, M, Din, "X")) return rc;
+    if (int rc = rows_checks(ctx, type, M, Dout, "Y")) return rc;
+    if (K < 1 || K > kGroupNodes) return fail(ctx, SOM_EINVAL, "K (%d) outside 1..%d", K, kGroupNodes);
+    if (!offsets && K != 1) return fail(ctx, SOM_EINVAL, "without offsets there is one node (K=%d)", K);
+    if (activation < SOM_ACT_NONE || activation > SOM_ACT_GELU_TANH) return fail(ctx, SOM_EINVAL, "unknown activation %d", activation);
+    if (int rc = array_check(ctx, offsets, K, false, "offsets")) return rc;
+    return matrix_check(ctx, A, needs_A ? 1 : 0, Din, Din, type, true, "A");
+}
+
+int som_node_product(som_ctx* ctx, int type, const void* X, int64_t M, int32_t Din, int64_t ldx, const int32_t* offsets, int32_t K, const void* A,
+                     int32_t Dout, const void* bias, int activation, const void* residual, int64_t ldr, void* pre, int64_t ldpre, void* Y, int64_t ldy)
+{
+    if (!ctx) return SOM_EINVAL;
+    if (int rc = models_checks(ctx, type, M, Din, Dout, offsets, K, A, true, activation)) return rc;
+    if (int rc = matrix_check(ctx, X, M, Din, ldx, type, true, "X")) return rc;
+    if (int rc = matrix_check(ctx, Y, M, Dout, ldy, type, true, "Y")) return rc;
+    if (int rc = matrix_check(ctx, bias, 1, Dout, Dout, type, false, "bias")) return rc;
+    if (int rc = matrix_check(ctx, residual, M, Dout, ldr, type, false, "residual")) return rc;
+    if (int rc = matrix_check(ctx, pre, M, Dout, ldpre, type, false, "pre")) return rc;
+    if (int rc = check_hip(ctx, hipSetDevice(ctx->device), "hipSetDevice")) return rc;
+    NodeProduct p{X, M, Din, ldx, offsets, K, A, Dout, bias, activation, residual, ldr, pre, ldpre, Y, ldy};
+    return node_product_run(ctx, type, p);
+}
+
+int som_node_product_grad(som_ctx* ctx, int type, const void* dY, int64_t M, int32_t Dout, int64_t lddy, const void* X, int32_t Din, int64_t ldx,
+                          const int32_t* offsets, int32_t K, const void* A, const void* pre, int64_t ldpre, int activation, void* dX, int64_t lddx,
+                          void* dA, void* dbias)
+{
+    if (!ctx) return SOM_EINVAL;
+    if (int rc = models_checks(ctx, type, M, Din, Dout, offsets, K, A, dX != nullptr, activation)) return rc;
+    if (!dX && !dA && !dbias) return fail(ctx, SOM_EINVAL, "none of dX, dA and dbias is asked for");
+    if (int rc = matrix_check(ctx, dY, M, Dout, lddy, type, true, "dY")) return rc;
+    if (int rc = matrix_check(ctx, X, dA ? M : 0, Din, ldx, type, true, "X")) return rc;
+    if (int rc = matrix_check(ctx, pre, activation != SOM_ACT_NONE ? M : 0, Dout, ldpre, type, true, "pre")) return rc;
+    if (int rc = matrix_check(ctx, dX, M, Din, lddx, type, false, "dX")) return rc;
+    if (int rc = matrix_check(ctx, dA, 1, Din, Din, type, false, "dA")) return rc;
+    if (int rc = matrix_check(ctx, dbias, 1, Dout, Dout, type, false, "dbias")) return rc;
+    if (int rc = check_hip(ctx, hipSetDevice(ctx->device), "hipSetDevice")) return rc;
+    NodeProductGrad p{dY, M, Dout, lddy, X, Din, ldx, offsets, K, A, pre, ldpre, activation, dX, lddx, dA, dbias};
+    return node_product_grad_run(ctx, type, p);
 }
 
 // host mirror of the small device-side results

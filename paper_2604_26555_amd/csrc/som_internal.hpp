@@ -142,6 +142,8 @@ struct som_ctx {
     int small_turn = 0;
     void* topo_blob = nullptr;     // node distances, adjacency matrix and lists of the topology rebuild
     size_t topo_bytes = 0;
+    void* models_blob = nullptr;   // counts of the sort of (row, node) pairs; gradients before the activation
+    size_t models_bytes = 0;
     // epoch-internal accumulators
     double* S = nullptr;
     size_t S_elems = 0;
@@ -207,5 +209,58 @@ int update_run(som_ctx* ctx, const double* S, const unsigned long long* n, const
 int update_static_init(som_ctx* ctx);
 int update_static_run(som_ctx* ctx, const double* S, const unsigned long long* n, const float* G, int32_t K,
                       int32_t D, double sigma, double eps_h, float* W, int32_t* small);
+
+// local models: rows sorted by node and back (som_group.hip)
+constexpr int kGroupNodes = 32768;              // nodes at most: a wavefront's counters of the sort in LDS
+constexpr int kModelWidth = 1 << 20;            // features of a row, and
+constexpr int kModelStride = 1 << 21;           // leading dimension, at most: offsets inside a tile of rows have 32 bits
+int models_workspace(som_ctx* ctx, size_t bytes);
+int group_run(som_ctx* ctx, const int32_t* node, int64_t pairs, int32_t K, int32_t* offsets, int32_t* order, int32_t* slot);
+int dispatch_run(som_ctx* ctx, int type, const void* X, int64_t rows, int32_t D, int64_t ldx, const int32_t* slot, int32_t k, const float* weight,
+                 void* Y, int64_t places, int64_t ldy);
+int combine_run(som_ctx* ctx, int type, const void* Y, int64_t places, int32_t D, int64_t ldy, const int32_t* slot, int64_t rows, int32_t k,
+                const float* weight, void* out, int64_t ldo);
+int combine_grad_run(som_ctx* ctx, int type, const void* dout, int64_t rows, int32_t D, int64_t lddo, const void* Y, int64_t places, int64_t ldy,
+                     const int32_t* slot, int32_t k, const float* weight, void* dY, int64_t lddy, float* dweight);
+// products with the nodes' matrices (som_product.hip)
+struct NodeProduct {
+    const void* X;
+    int64_t rows;
+    int32_t din;
+    int64_t ldx;
+    const int32_t* offsets;
+    int32_t K;
+    const void* A;
+    int32_t dout;
+    const void* bias;
+    int act;
+    const void* residual;
+    int64_t ldr;
+    void* pre;
+    int64_t ldpre;
+    void* out;
+    int64_t ldo;
+};
+struct NodeProductGrad {
+    const void* dY;
+    int64_t rows;
+    int32_t dout;
+    int64_t lddy;
+    const void* X;
+    int32_t din;
+    int64_t ldx;
+    const int32_t* offsets;
+    int32_t K;
+    const void* A;
+    const void* pre;
+    int64_t ldpre;
+    int act;
+    void* dX;
+    int64_t lddx;
+    void* dA;
+    void* dbias;
+};
+int node_product_run(som_ctx* ctx, int type, const NodeProduct& p);
+int node_product_grad_run(som_ctx* ctx, int type, const NodeProductGrad& p);
 
 } // namespace som

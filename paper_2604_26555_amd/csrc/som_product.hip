@@ -1,0 +1,370 @@
+// One matrix per node: every row of a node's group times that node's matrix, and the gradient.
+//
+//   product    z_s = A_e x_s + c_e,  y_s = act(z_s) + r_s                                          for s in group e
+//   gradient   dz_s = dy_s act'(z_s);  dx_s = A_e^T dz_s,  dA_e = sum_s dz_s x_s^T,  dc_e = sum_s dz_s
+//
+// Rows of group e are offsets[e] .. offsets[e + 1] - 1 (no offsets: one node, all rows).  The group's bounds are on the device,
+// so a launch covers as many tiles as there can be and every workgroup looks up its own.  Products of 16-bit rows and their
+// sums are taken by the matrix pipe in float32; float32 rows go through its float32 form.
+#include "som_rows.hpp"
+
+namespace som {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// What a tile of the contraction is made of: C[m][n] = sum_k P[m][k] Q[n][k].
+enum Form {
+    kRowsTimesA,        // m: rows of X, n: results, k: features
+    kRowsTimesAt,       // m: rows of dz, n: features, k: results
+    kOuterSums          // m: results, n: features, k: rows of the group
+};
+
+template <class T>
+struct ProductArgs {
+    const T* P;                // X, dz, dz
+    int64_t ldp;
+    const T* Q;                // A, A, X
+    int64_t ldq;               // X only
+    const int32_t* offsets;    // null: one node
+    int64_t rows;
+    int32_t K, din, dout;
+    const T* bias;
+    const T* residual;
+    int64_t ldr;
+    T* pre;
+    int64_t ldpre;
+    T* out;                    // Y, dX, dA
+    int64_t ldo;
+    int act;
+};
+
+// Where a factor has reached its limit the product with z is formed from the limit, so that infinities give what the function
+// tends to.  The error function's complement keeps the small values of the left tail to their last places.
+__device__ __forceinline__ float activate(float z, int act)
+{
+    switch (act) {
+    case SOM_ACT_RELU: return z < 0.0f ? 0.0f : z;                       // (a NaN stays one)
+    case SOM_ACT_SILU: return z < -110.0f ? 0.0f : z / (1.0f + expf(-z));
+    case SOM_ACT_GELU: return z < -30.0f ? 0.0f : 0.5f * z * erfcf(-0.70710678f * z);
+    case SOM_ACT_GELU_TANH:                                             // (1 + tanh u) / 2 = 1 / (1 + exp(-2 u))
+        return z < -30.0f ? 0.0f : z > 30.0f ? z : z / (1.0f + expf(-1.59576912f * (z + 0.044715f * z * z * z)));
+    }
+    return z;
+}
+
+__device__ __forceinline__ float slope(float z, int act)
+{
+    switch (act) {
+    case SOM_ACT_RELU: return z > 0.0f ? 1.0f : z == z ? 0.0f : z;
+    case SOM_ACT_SILU: {
+        if (fabsf(z) > 110.0f) return z > 0.0f ? 1.0f : 0.0f;
+        const float g = 1.0f / (1.0f + expf(-z));
+        return g * (1.0f + z * (1.0f - g));
+    }
+    case SOM_ACT_GELU:
+        if (fabsf(z) > 30.0f) return z > 0.0f ? 1.0f : 0.0f;
+        return 0.5f * erfcf(-0.70710678f * z) + z * expf(-0.5f * z * z) * 0.39894228f;
+    case SOM_ACT_GELU_TANH: {
+        if (fabsf(z) > 30.0f) return z > 0.0f ? 1.0f : 0.0f;
+        const float g = 1.0f / (1.0f + expf(-1.59576912f * (z + 0.044715f * z * z * z)));
+        return g * (1.0f + z * (1.0f - g) * 1.59576912f * (1.0f + 0.134145f * z * z));
+    }
+    }
+    return 1.0f;
+}
+
+// Rows [lo, hi) of group e, inside [0, rows) whatever the offsets hold.
+__device__ __forceinline__ void group_rows(const int32_t* __restrict__ offsets, int e, int64_t rows, int64_t& lo, int64_t& hi)
+{
+    if (!offsets) {
+        lo = 0;
+        hi = rows;
+        return;
+    }
+    lo = offsets[e];
+    hi = offsets[e + 1];
+    lo = lo < 0 ? 0 : lo > rows ? rows : lo;
+    hi = hi < lo ? lo : hi > rows ? rows : hi;
+}
+
+// Tile `tile` of all groups' tiles of BM rows, in the groups' order: its group and its first row.  Called by a whole
+// workgroup; false when there are fewer tiles.
+template <int BM, int THREADS>
+__device__ __forceinline__ bool find_tile(const int32_t* __restrict__ offsets, int K, int64_t rows, int64_t tile, int& e, int64_t& first, int64_t& end)
+{
+    __shared__ int sums[THREADS / 64];
+    __shared__ int found[2];
+    if (!offsets) {
+        e = 0;
+        first = tile * BM;
+        end = rows;
+        return first < rows;
+    }
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    if (tid == 0) found[0] = -1;
+    int64_t before = 0;
+    for (int e0 = 0; e0 < K; e0 += THREADS) {
+        int64_t lo = 0, hi = 0;
+        if (e0 + tid < K) group_rows(offsets, e0 + tid, rows, lo, hi);
+        const int mine = (int)((hi - lo + BM - 1) / BM);
+        int incl = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int x = __shfl_up(incl, o);
+            if (lane >= o) incl += x;
+        }
+        __syncthreads();                          // sums and found of the round before have been read
+        if (lane == 63) sums[wave] = incl;
+        __syncthreads();
+        int64_t at = before + incl - mine;
+        for (int w = 0; w < THREADS / 64; ++w) {
+            if (w < wave) at += sums[w];
+            before += sums[w];
+        }
+        if (tile >= at && tile < at + mine) {
+            found[0] = e0 + tid;
+            found[1] = (int)(tile - at);
+        }
+        if (before > tile) break;
+    }
+    __syncthreads();
+    if (found[0] < 0) return false;
+    e = found[0];
+    int64_t lo;
+    group_rows(offsets, e, rows, lo, end);
+    first = lo + (int64_t)found[1] * BM;
+    return true;
+}
+
+__device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mfma(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+
+template <class T>
+struct Half8;
+template <>
+struct Half8<__bf16> {
+    typedef bf16x8 type;
+};
+template <>
+struct Half8<_Float16> {
+    typedef f16x8 type;
+};
+
+// Tiles of 64 x 64 in four wavefronts of 32 x 32, operands through LDS a value at a time: any shape, stride and alignment.
+template <class T, Form F>
+__global__ void __launch_bounds__(256) product_any_kernel(ProductArgs<T> a)
+{
+    constexpr int BM = 64, BN = 64, BK = 32, PAD = sizeof(T) == 2 ? 8 : 1;
+    __shared__ __align__(16) T P[BM][BK + PAD], Q[BN][BK + PAD];
+    const int M = F == kOuterSums ? a.dout : 0, Nn = F == kRowsTimesA ? a.dout : a.din;
+    int e;
+    int64_t first, end;
+    int64_t m0;
+    if (F == kOuterSums) {
+        e = blockIdx.z;
+        m0 = (int64_t)blockIdx.y * BM;
+        group_rows(a.offsets, e, a.rows, first, end);
+    } else {
+        if (!find_tile<BM, 256>(a.offsets, a.K, a.rows, (int64_t)blockIdx.y + (int64_t)blockIdx.z * gridDim.y, e, first, end)) return;
+        m0 = 0;
+    }
+    const int n0 = blockIdx.x * BN;
+    const T* A = F == kOuterSums ? nullptr : a.Q + (int64_t)e * a.dout * a.din;
+    const int64_t depth = F == kRowsTimesA ? a.din : F == kRowsTimesAt ? a.dout : end - first;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int wm = (wave & 1) * 32, wn = (wave >> 1) * 32;
+    f32x16 acc = {};
+    for (int64_t k0 = 0; k0 < depth; k0 += BK) {
+        __syncthreads();
+        for (int i = threadIdx.x; i < BM * BK; i += 256) {
+            if (F == kOuterSums) {                                   // consecutive lanes take consecutive m
+                const int m = i % BM, k = i / BM;
+                P[m][k] = m0 + m < M && k0 + k < depth ? a.P[(first + k0 + k) * a.ldp + m0 + m] : (T)0.0f;
+            } else {
+                const int k = i % BK, m = i / BK;
+                P[m][k] = first + m < end && k0 + k < depth ? a.P[(first + m) * a.ldp + k0 + k] : (T)0.0f;
+            }
+        }
+        for (int i = threadIdx.x; i < BN * BK; i += 256) {
+            if (F == kRowsTimesA) {
+                const int k = i % BK, n = i / BK;
+                Q[n][k] = n0 + n < Nn && k0 + k < depth ? A[(int64_t)(n0 + n) * a.din + k0 + k] : (T)0.0f;
+            } else {
+                const int n = i % BN, k = i / BN;
+                const T* row = F == kRowsTimesAt ? A + (k0 + k) * a.din : a.Q + (first + k0 + k) * a.ldq;
+                Q[n][k] = n0 + n < Nn && k0 + k < depth ? row[n0 + n] : (T)0.0f;
+            }
+        }
+        __syncthreads();
+        if constexpr (sizeof(T) == 2) {
+            typedef typename Half8<T>::type half8;
+#pragma unroll
+            for (int q = 0; q < BK; q += 16) {
+                const half8 p = *reinterpret_cast<const half8*>(&P[wm + (lane & 31)][q + 8 * (lane >> 5)]);
+                const half8 r = *reinterpret_cast<const half8*>(&Q[wn + (lane & 31)][q + 8 * (lane >> 5)]);
+                acc = mfma(p, r, acc);
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < BK; q += 2)
+                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(P[wm + (lane & 31)][q + (lane >> 5)], Q[wn + (lane & 31)][q + (lane >> 5)], acc, 0, 0, 0);
+        }
+    }
+    const int n = n0 + wn + (lane & 31);
+    if (n >= Nn) return;
+    const float c = F == kRowsTimesA && a.bias ? (float)a.bias[(int64_t)e * a.dout + n] : 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const int m = wm + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5);
+        float z = acc[r];
+        if (F == kOuterSums) {
+            if (m0 + m < M) a.out[((int64_t)e * a.dout + m0 + m) * a.din + n] = (T)z;
+            continue;
+        }
+        const int64_t s = first + m;
+        if (s >= end) continue;
+        if (F == kRowsTimesA) {
+            z += c;
+            if (a.pre) a.pre[s * a.ldpre + n] = (T)z;
+            z = activate(z, a.act);
+            if (a.residual) z += (float)a.residual[s * a.ldr + n];
+        }
+        a.out[s * a.ldo + n] = (T)z;
+    }
+}
+
+// dz = dy act'(z), dense
+template <class T>
+__global__ void __launch_bounds__(256) slope_kernel(const T* __restrict__ dY, int64_t lddy, const T* __restrict__ pre, int64_t ldpre, int64_t rows,
+                                                    int32_t dout, int act, T* __restrict__ dz)
+{
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * dout; i += (int64_t)gridDim.x * 256) {
+        const int64_t s = i / dout;
+        const int n = (int)(i - s * dout);
+        dz[i] = (T)((float)dY[s * lddy + n] * slope((float)pre[s * ldpre + n], act));
+    }
+}
+
+// dc_e: 64 results and 4 runs of rows per workgroup
+template <class T>
+__global__ void __launch_bounds__(256) bias_grad_kernel(const T* __restrict__ dz, int64_t lddz, const int32_t* __restrict__ offsets, int64_t rows,
+                                                        int32_t dout, T* __restrict__ dbias)
+{
+    __shared__ float run[4][64];
+    const int e = blockIdx.y, l = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockIdx.x * 64 + l;
+    int64_t lo, hi;
+    group_rows(offsets, e, rows, lo, hi);
+    float s = 0.0f;
+    if (n < dout)
+        for (int64_t r = lo + wave; r < hi; r += 4) s += (float)dz[r * lddz + n];
+    run[wave][l] = s;
+    __syncthreads();
+    if (wave == 0 && n < dout) dbias[(int64_t)e * dout + n] = (T)((run[0][l] + run[1][l]) + (run[2][l] + run[3][l]));
+}
+
+// Tiles of `bm` rows that the groups can have together.
+static int64_t most_tiles(int64_t rows, int32_t K, const int32_t* offsets, int bm)
+{
+    const int64_t full = (rows + bm - 1) / bm;
+    return offsets ? full + (K < rows ? K : rows) : full;
+}
+
+template <class T, Form F>
+static int product_launch(som_ctx* ctx, const ProductArgs<T>& a, const char* what)
+{
+    const unsigned nx = (unsigned)(((F == kRowsTimesA ? a.dout : a.din) + 63) / 64);
+    dim3 grid;
+    if (F == kOuterSums) {
+        grid = dim3(nx, (unsigned)((a.dout + 63) / 64), (unsigned)a.K);
+    } else {
+        const int64_t tiles = most_tiles(a.rows, a.K, a.offsets, 64);
+        const int64_t y = tiles < 32768 ? tiles : 32768;
+        grid = dim3(nx, (unsigned)y, (unsigned)((tiles + y - 1) / y));
+    }
+    hipLaunchKernelGGL((product_any_kernel<T, F>), grid, dim3(256), 0, ctx->stream, a);
+    return check_hip(ctx, hipGetLastError(), what);
+}
+
+template <class T>
+static int product_typed(som_ctx* ctx, const NodeProduct& p)
+{
+    ProductArgs<T> a{};
+    a.P = (const T*)p.X;
+    a.ldp = p.ldx;
+    a.Q = (const T*)p.A;
+    a.offsets = p.offsets;
+    a.rows = p.rows;
+    a.K = p.K;
+    a.din = p.din;
+    a.dout = p.dout;
+    a.bias = (const T*)p.bias;
+    a.residual = (const T*)p.residual;
+    a.ldr = p.ldr;
+    a.pre = (T*)p.pre;
+    a.ldpre = p.ldpre;
+    a.out = (T*)p.out;
+    a.ldo = p.ldo;
+    a.act = p.act;
+    return product_launch<T, kRowsTimesA>(ctx, a, "product launch");
+}
+
+template <class T>
+static int product_grad_typed(som_ctx* ctx, const NodeProductGrad& p)
+{
+    const T* dz = (const T*)p.dY;
+    int64_t lddz = p.lddy;
+    if (p.act != SOM_ACT_NONE && p.rows > 0) {
+        if (int rc = models_workspace(ctx, (size_t)p.rows * p.dout * sizeof(T))) return rc;
+        const int64_t groups = (p.rows * p.dout + 255) / 256;
+        hipLaunchKernelGGL(slope_kernel<T>, dim3((unsigned)(groups < 65536 ? groups : 65536)), dim3(256), 0, ctx->stream, (const T*)p.dY, p.lddy,
+                           (const T*)p.pre, p.ldpre, p.rows, p.dout, p.act, (T*)ctx->models_blob);
+        if (int rc = check_hip(ctx, hipGetLastError(), "product gradient slope launch")) return rc;
+        dz = (const T*)ctx->models_blob;
+        lddz = p.dout;
+    }
+    ProductArgs<T> a{};
+    a.P = dz;
+    a.ldp = lddz;
+    a.offsets = p.offsets;
+    a.rows = p.rows;
+    a.K = p.K;
+    a.din = p.din;
+    a.dout = p.dout;
+    if (p.dX && p.rows > 0) {
+        a.Q = (const T*)p.A;
+        a.out = (T*)p.dX;
+        a.ldo = p.lddx;
+        if (int rc = product_launch<T, kRowsTimesAt>(ctx, a, "product gradient (rows) launch")) return rc;
+    }
+    if (p.dA) {
+        a.Q = (const T*)p.X;
+        a.ldq = p.ldx;
+        a.out = (T*)p.dA;
+        if (int rc = product_launch<T, kOuterSums>(ctx, a, "product gradient (matrices) launch")) return rc;
+    }
+    if (p.dbias) {
+        hipLaunchKernelGGL(bias_grad_kernel<T>, dim3((unsigned)((p.dout + 63) / 64), (unsigned)p.K), dim3(256), 0, ctx->stream, dz, lddz, p.offsets,
+                           p.rows, p.dout, (T*)p.dbias);
+        if (int rc = check_hip(ctx, hipGetLastError(), "product gradient (biases) launch")) return rc;
+    }
+    return SOM_OK;
+}
+
+int node_product_run(som_ctx* ctx, int type, const NodeProduct& p)
+{
+    if (p.rows == 0) return SOM_OK;
+    if (type == SOM_ROWS_FLOAT) return product_typed<float>(ctx, p);
+    if (type == SOM_ROWS_BFLOAT) return product_typed<__bf16>(ctx, p);
+    return product_typed<_Float16>(ctx, p);
+}
+
+int node_product_grad_run(som_ctx* ctx, int type, const NodeProductGrad& p)
+{
+    if (type == SOM_ROWS_FLOAT) return product_grad_typed<float>(ctx, p);
+    if (type == SOM_ROWS_BFLOAT) return product_grad_typed<__bf16>(ctx, p);
+    return product_grad_typed<_Float16>(ctx, p);
+}
+
+} // namespace som

@@ -25,12 +25,15 @@ SOM_SEARCH_AUTO = 0
 SOM_SEARCH_FLOAT32 = 1
 SOM_TOPOLOGY_MST = 1
 SOM_TOPOLOGY_RNG = 2
+SOM_ROWS_FLOAT, SOM_ROWS_BFLOAT, SOM_ROWS_HALF = 0, 1, 2
+SOM_ACT_NONE, SOM_ACT_RELU, SOM_ACT_SILU, SOM_ACT_GELU, SOM_ACT_GELU_TANH = 0, 1, 2, 3, 4
 
 EXPORTS = [
     "som_create", "som_destroy", "som_strerror", "som_last_error", "som_sync", "som_bmu", "som_accumulate",
     "som_neighborhood_update", "som_epoch", "som_epoch_host", "som_profile", "som_profile_read",
     "som_set_update_rule", "som_topology", "som_set_safeguard", "som_set_reproducible", "som_set_search",
     "som_matrix_pipe_probe", "som_matrix_pipe_probe_parts", "som_neighborhood_update_static", "som_epoch_file", "som_read_probe", "som_mfma_rate_probe",
+    "som_group", "som_dispatch", "som_combine", "som_combine_grad", "som_node_product", "som_node_product_grad",
 ]
 
 
@@ -107,6 +110,18 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     lib.som_read_probe.restype = C.c_int
     lib.som_epoch_file.argtypes = [vp, C.c_int, i64, i64, i32, i64, vp, i32, vp, f64, C.c_int, f64, C.POINTER(SomStats)]
     lib.som_epoch_file.restype = C.c_int
+    lib.som_group.argtypes = [vp, vp, i64, i32, i32, vp, vp, vp]
+    lib.som_group.restype = C.c_int
+    lib.som_dispatch.argtypes = [vp, C.c_int, vp, i64, i32, i64, vp, i32, vp, vp, i64, i64]
+    lib.som_dispatch.restype = C.c_int
+    lib.som_combine.argtypes = [vp, C.c_int, vp, i64, i32, i64, vp, i64, i32, vp, vp, i64]
+    lib.som_combine.restype = C.c_int
+    lib.som_combine_grad.argtypes = [vp, C.c_int, vp, i64, i32, i64, vp, i64, i64, vp, i32, vp, vp, i64, vp]
+    lib.som_combine_grad.restype = C.c_int
+    lib.som_node_product.argtypes = [vp, C.c_int, vp, i64, i32, i64, vp, i32, vp, i32, vp, C.c_int, vp, i64, vp, i64, vp, i64]
+    lib.som_node_product.restype = C.c_int
+    lib.som_node_product_grad.argtypes = [vp, C.c_int, vp, i64, i32, i64, vp, i32, i64, vp, i32, vp, vp, i64, C.c_int, vp, i64, vp, vp]
+    lib.som_node_product_grad.restype = C.c_int
     _lib = lib
     return lib
 
@@ -136,6 +151,10 @@ def _matrix(t: torch.Tensor, name: str):
         raise ValueError(f"{name} must be a row-major 2-D tensor")
     (rows, columns), ld = shape, stride[0]
     return rows, columns, ld if rows > 1 else max(columns, ld)
+
+
+_ROWS = {torch.float32: SOM_ROWS_FLOAT, torch.bfloat16: SOM_ROWS_BFLOAT, torch.float16: SOM_ROWS_HALF}
+_ACTIVATIONS = {"none": SOM_ACT_NONE, "relu": SOM_ACT_RELU, "silu": SOM_ACT_SILU, "gelu": SOM_ACT_GELU, "gelu_tanh": SOM_ACT_GELU_TANH}
 
 
 @dataclass
@@ -351,6 +370,186 @@ class Som:
                                    _ptr(G, torch.float32, "G", self.device))
         self._check(rc, "som_topology")
         return G
+
+    # ------------------------------------------------------------------ local models: one matrix per node
+    def _empty(self, shape, dtype):
+        """A new tensor that this context's stream may write at once: its memory comes from that stream's pool."""
+        if torch.cuda.current_stream(self.device) == self.stream:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(self.stream):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def _rows(self, t, name, dtype=None, shape=None):
+        """(address, rows, columns, leading dimension) of a matrix of a local model's rows."""
+        if dtype is not None and t.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+        if t.dtype not in _ROWS:
+            raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+        if t.device != self.device:
+            raise ValueError(f"{name} lives on {t.device}, the context is on {self.device}")
+        rows, columns, ld = _matrix(t, name)
+        if shape is not None and (rows, columns) != shape:
+            raise ValueError(f"{name} must be {shape[0]} x {shape[1]}, got {rows} x {columns}")
+        return t.data_ptr(), rows, columns, ld
+
+    def _pairs(self, t, name, dtype):
+        """(address, rows, nodes per row) of an array with an entry for each pair of row and node: (T,) or (T, k)."""
+        if t.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+        if t.device != self.device:
+            raise ValueError(f"{name} lives on {t.device}, the context is on {self.device}")
+        if t.dim() not in (1, 2) or not t.is_contiguous() or (t.dim() == 2 and t.shape[1] < 1):
+            raise ValueError(f"{name} must be a contiguous (T,) or (T, k) tensor")
+        return t.data_ptr(), t.shape[0], t.shape[1] if t.dim() == 2 else 1
+
+    def _weights(self, weight, slot):
+        if weight is None:
+            return None
+        if weight.shape != slot.shape:
+            raise ValueError("weight must have slot's shape")
+        return self._pairs(weight, "weight", torch.float32)[0]
+
+    def _nodes(self, X, A, offsets):
+        """(K, Dout, Din, address of the offsets) of the nodes' matrices A: (K, Dout, Din), or (Dout, Din) without offsets."""
+        shape = A.shape if A.dim() == 3 else (1, *A.shape)
+        if len(shape) != 3 or not A.is_contiguous():
+            raise ValueError("A must be a contiguous (K, Dout, Din) or, for one node, (Dout, Din) tensor")
+        if A.dtype != X.dtype:
+            raise TypeError(f"A must be {X.dtype}, got {A.dtype}")
+        if A.device != self.device:
+            raise ValueError(f"A lives on {A.device}, the context is on {self.device}")
+        if offsets is None:
+            if shape[0] != 1:
+                raise ValueError("without offsets there is one node")
+        elif offsets.numel() != shape[0] + 1 or offsets.dim() != 1:
+            raise ValueError("offsets must have K + 1 entries")
+        return (*shape, _ptr(offsets, torch.int32, "offsets", self.device))
+
+    def _bias(self, t, name, A, K, Dout):
+        if t.numel() != K * Dout or t.shape[-1] != Dout or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous K x Dout tensor")
+        return _ptr(t, A.dtype, name, self.device)
+
+    def som_group(self, node, K, offsets=None, order=None, slot=None):
+        """Sorts the pairs of row and node by node, stably; node: int32 (T,) or (T, k), entries outside [0, K) have no place.
+        Returns (offsets (K + 1), order (T k), slot (node's shape)): node e has places offsets[e] .. offsets[e + 1] - 1, order
+        holds the pair t * k + j at each place, slot the place of each pair; -1 stands for none."""
+        at, T, k = self._pairs(node, "node", torch.int32)
+        if offsets is None:
+            offsets = self._empty(int(K) + 1, torch.int32)
+        elif offsets.numel() != int(K) + 1:
+            raise ValueError("offsets must have K + 1 entries")
+        if order is None:
+            order = self._empty(T * k, torch.int32)
+        elif order.numel() != T * k or order.dim() != 1:
+            raise ValueError("order must have one entry per pair")
+        if slot is None:
+            slot = self._empty(node.shape, torch.int32)
+        elif slot.shape != node.shape:
+            raise ValueError("slot must have node's shape")
+        rc = self.lib.som_group(self._h, at, T, k, int(K), _ptr(offsets, torch.int32, "offsets", self.device),
+                                _ptr(order, torch.int32, "order", self.device), self._pairs(slot, "slot", torch.int32)[0])
+        self._check(rc, "som_group")
+        return offsets, order, slot
+
+    def som_dispatch(self, X, slot, weight=None, out=None):
+        """Rows to their places: out[slot[t, j]] = weight[t, j] * X[t] (without weights: X[t]).  out: T k rows unless given;
+        rows that are no pair's place are left as they were."""
+        x, T, D, ldx = self._rows(X, "X")
+        s, Ts, k = self._pairs(slot, "slot", torch.int32)
+        if Ts != T:
+            raise ValueError("slot must have one row per row of X")
+        if out is None:
+            out = self._empty((T * k, D), X.dtype)
+        y, M, Dy, ldy = self._rows(out, "out", X.dtype)
+        if Dy != D:
+            raise ValueError("out must have X's width")
+        rc = self.lib.som_dispatch(self._h, _ROWS[X.dtype], x, T, D, ldx, s, k, self._weights(weight, slot), y, M, ldy)
+        self._check(rc, "som_dispatch")
+        return out
+
+    def som_combine(self, Y, slot, weight=None, out=None):
+        """Rows back: out[t] = sum_j weight[t, j] * Y[slot[t, j]]."""
+        y, M, D, ldy = self._rows(Y, "Y")
+        s, T, k = self._pairs(slot, "slot", torch.int32)
+        if out is None:
+            out = self._empty((T, D), Y.dtype)
+        o, _, _, ldo = self._rows(out, "out", Y.dtype, (T, D))
+        rc = self.lib.som_combine(self._h, _ROWS[Y.dtype], y, M, D, ldy, s, T, k, self._weights(weight, slot), o, ldo)
+        self._check(rc, "som_combine")
+        return out
+
+    def som_combine_grad(self, dout, Y, slot, weight=None, dY=None, dweight=None):
+        """Gradient of som_combine: (dY, dweight).  Either is left out, and returned as None, where False is given for it."""
+        y, M, D, ldy = self._rows(Y, "Y")
+        s, T, k = self._pairs(slot, "slot", torch.int32)
+        g, _, _, lddo = self._rows(dout, "dout", Y.dtype, (T, D))
+        dy = lddy = dw = None
+        if dY is None:
+            dY = self._empty((M, D), Y.dtype)
+        if dY is not False:
+            dy, _, _, lddy = self._rows(dY, "dY", Y.dtype, (M, D))
+        if dweight is None:
+            dweight = self._empty(slot.shape, torch.float32)
+        if dweight is not False:
+            if dweight.shape != slot.shape:
+                raise ValueError("dweight must have slot's shape")
+            dw = self._pairs(dweight, "dweight", torch.float32)[0]
+        rc = self.lib.som_combine_grad(self._h, _ROWS[Y.dtype], g, T, D, lddo, y, M, ldy, s, k, self._weights(weight, slot), dy, lddy or D, dw)
+        self._check(rc, "som_combine_grad")
+        return (dY if dY is not False else None), (dweight if dweight is not False else None)
+
+    def som_node_product(self, X, A, offsets=None, bias=None, activation="none", residual=None, pre=None, out=None):
+        """Every row times its node's matrix: out[s] = activation(A[e] X[s] + bias[e]) + residual[s] for the rows
+        offsets[e] <= s < offsets[e + 1] of node e; without offsets A is one matrix for all rows.  pre, if given, receives the values
+        before the activation.  activation: none, relu, silu, gelu or gelu_tanh."""
+        x, M, Din, ldx = self._rows(X, "X")
+        K, Dout, Da, off = self._nodes(X, A, offsets)
+        if Da != Din:
+            raise ValueError("A must have X's width")
+        c = None if bias is None else self._bias(bias, "bias", A, K, Dout)
+        r = ldr = z = ldz = None
+        if residual is not None:
+            r, _, _, ldr = self._rows(residual, "residual", X.dtype, (M, Dout))
+        if pre is not None:
+            z, _, _, ldz = self._rows(pre, "pre", X.dtype, (M, Dout))
+        if out is None:
+            out = self._empty((M, Dout), X.dtype)
+        y, _, _, ldy = self._rows(out, "out", X.dtype, (M, Dout))
+        rc = self.lib.som_node_product(self._h, _ROWS[X.dtype], x, M, Din, ldx, off, K, A.data_ptr(), Dout, c, _ACTIVATIONS[activation], r, ldr or Dout,
+                                       z, ldz or Dout, y, ldy)
+        self._check(rc, "som_node_product")
+        return out
+
+    def som_node_product_grad(self, dY, X, A, offsets=None, pre=None, activation="none", dX=None, dA=None, dbias=None):
+        """Gradient of som_node_product: (dX, dA, dbias); pre as som_node_product filled it, needed where there is an activation.
+        Each is left out, and returned as None, where False is given for it.  The residual's gradient is dY."""
+        x, M, Din, ldx = self._rows(X, "X")
+        K, Dout, Da, off = self._nodes(X, A, offsets)
+        if Da != Din:
+            raise ValueError("A must have X's width")
+        g, _, _, lddy = self._rows(dY, "dY", X.dtype, (M, Dout))
+        z = ldz = dx = lddx = da = dc = None
+        if pre is not None:
+            z, _, _, ldz = self._rows(pre, "pre", X.dtype, (M, Dout))
+        if dX is None:
+            dX = self._empty((M, Din), X.dtype)
+        if dX is not False:
+            dx, _, _, lddx = self._rows(dX, "dX", X.dtype, (M, Din))
+        if dA is None:
+            dA = self._empty(A.shape, X.dtype)
+        if dA is not False:
+            if dA.shape != A.shape or not dA.is_contiguous():
+                raise ValueError("dA must be contiguous and have A's shape")
+            da = _ptr(dA, X.dtype, "dA", self.device)
+        if dbias is None:
+            dbias = self._empty((*A.shape[:-2], Dout), X.dtype)
+        if dbias is not False:
+            dc = self._bias(dbias, "dbias", A, K, Dout)
+        rc = self.lib.som_node_product_grad(self._h, _ROWS[X.dtype], g, M, Dout, lddy, x, Din, ldx, off, K, A.data_ptr(), z, ldz or Dout,
+                                            _ACTIVATIONS[activation], dx, lddx or Din, da, dc)
+        self._check(rc, "som_node_product_grad")
+        return tuple(None if t is False else t for t in (dX, dA, dbias))
 
     # ------------------------------------------------------------------ whole epoch
     def som_epoch(self, X, W, G, sigma, idx=None, eps_h=0.0, want_stats=True, kernel=SOM_KERNEL_GAUSSIAN):

@@ -1,0 +1,391 @@
+"""Local models on the GPU against the float64 reference: rows sorted by node and back, products with the nodes' matrices, gradients."""
+import math
+
+import pytest
+import torch
+
+import models_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def som():
+    from paper_2604_26555_amd import Som
+    s = Som(0)
+    yield s
+    s.close()
+
+
+def normal(gen, *shape, dtype=torch.float32, scale=1.0):
+    return (torch.randn(*shape, generator=gen) * scale).to(dtype)
+
+
+def padded(t, extra=0, lead=0):
+    """The same matrix on the GPU with a leading dimension of its own and an offset of `lead` elements."""
+    rows, cols = t.shape
+    buf = torch.full((rows * (cols + extra) + lead + 8,), float("nan"), dtype=t.dtype, device="cuda")
+    view = buf[lead:lead + rows * (cols + extra)].view(rows, cols + extra)[:, :cols]
+    view.copy_(t)
+    return view
+
+
+def draw_nodes(gen, T, k, K, how="even"):
+    if how == "one":
+        return torch.full((T, k), min(3, K - 1), dtype=torch.int32)
+    if how == "none":
+        return torch.full((T, k), -1, dtype=torch.int32)
+    node = torch.randint(0, K, (T, k), generator=gen)
+    if how == "skew":
+        node = (torch.rand(T, k, generator=gen) ** 6 * K).long().clamp(max=K - 1)
+    if how == "holes":
+        node = torch.where(torch.rand(T, k, generator=gen) < 0.2, torch.randint(-5, 0, (T, k), generator=gen), node)
+        node = torch.where(torch.rand(T, k, generator=gen) < 0.1, torch.randint(K, K + 9, (T, k), generator=gen), node)
+        node[::7] = -1
+    return node.int()
+
+
+GROUPS = [(1, 1, 1, "even"), (1, 8, 128, "even"), (3, 2, 5, "none"), (63, 1, 2, "even"), (64, 1, 64, "one"), (65, 3, 7, "holes"), (257, 2, 1, "even"),
+          (1000, 8, 100, "holes"), (2048, 1, 1024, "skew"), (4099, 4, 61, "holes"), (9001, 1, 8192, "even"), (5000, 2, 32768, "holes"),
+          (70001, 2, 437, "skew"), (300_000, 1, 1024, "holes"), (100_000, 8, 3, "one"), (40_000, 1, 20_000, "skew")]
+
+
+@pytest.mark.parametrize("T, k, K, how", GROUPS)
+def test_group(som, T, k, K, how):
+    gen = torch.Generator().manual_seed(T + K)
+    node = draw_nodes(gen, T, k, K, how)
+    want = ref.group(node, K)
+    got = som.som_group(node.cuda(), K)
+    for g, w, name in zip(got, want, ("offsets", "order", "slot")):
+        assert torch.equal(g.cpu(), w), name
+    if k == 1:                                     # a plain list of units
+        offsets, order, slot = som.som_group(node[:, 0].contiguous().cuda(), K)
+        assert torch.equal(slot.cpu(), want[2][:, 0]) and torch.equal(order.cpu(), want[1]) and torch.equal(offsets.cpu(), want[0])
+
+
+def test_group_of_nothing(som):
+    offsets, order, slot = som.som_group(torch.empty((0, 4), dtype=torch.int32, device="cuda"), 9)
+    assert offsets.tolist() == [0] * 10 and order.numel() == 0 and slot.shape == (0, 4)
+
+
+#       T, k, K, D, extra, lead, how
+ROWS = [(1, 1, 1, 1, 0, 0, "even"), (1, 8, 16, 2048, 0, 0, "even"), (5, 2, 3, 3, 2, 1, "holes"), (7, 3, 4, 7, 0, 3, "even"), (33, 2, 9, 8, 0, 0, "holes"),
+        (19, 4, 6, 50, 0, 0, "skew"), (23, 1, 6, 51, 6, 5, "holes"), (64, 2, 8, 64, 8, 0, "even"), (12, 8, 40, 1001, 1, 1, "holes"), (9, 5, 7, 129, 0, 0, "none"),
+        (17, 2, 4, 4096, 0, 0, "one"), (6, 3, 9, 2600, 3, 2, "holes")]
+
+
+@pytest.mark.parametrize("dtype", ref.TYPES)
+@pytest.mark.parametrize("T, k, K, D, extra, lead, how", ROWS)
+def test_dispatch_combine_and_gradient(som, T, k, K, D, extra, lead, how, dtype):
+    gen = torch.Generator().manual_seed(D)
+    node = draw_nodes(gen, T, k, K, how)
+    _, _, slot = ref.group(node, K)
+    X, Y, dout = normal(gen, T, D, dtype=dtype), normal(gen, T * k + 2, D, dtype=dtype), normal(gen, T, D, dtype=dtype)
+    weight = torch.softmax(torch.randn(T, k, generator=gen), 1)
+    slot_d, weight_d = slot.cuda(), weight.cuda()
+    Xd, Yd, gd = padded(X, extra, lead), padded(Y, extra, lead), padded(dout, 0, lead)
+    before = normal(gen, T * k + 2, D, dtype=dtype)
+    for w, wd in ((None, None), (weight, weight_d)):
+        out = padded(before, extra, lead)
+        assert som.som_dispatch(Xd, slot_d, weight=wd, out=out) is out
+        want, bound = ref.dispatch(X, slot, w, before)
+        ref.check(out, want, bound, "dispatch")
+        ref.check(som.som_combine(Yd, slot_d, weight=wd), *ref.combine(Y, slot, w), "combine")
+        dY = padded(before, extra, lead)
+        dweight = som.som_combine_grad(gd, Yd, slot_d, weight=wd, dY=dY)[1]
+        want, bound, dw, dwb = ref.combine_grad(dout, Y, slot, w, before)
+        ref.check(dY, want, bound, "dY")
+        ref.check(dweight, dw, dwb, "dweight")
+        only_y, none = som.som_combine_grad(gd, Yd, slot_d, weight=wd, dY=padded(before, extra, lead), dweight=False)
+        assert none is None and torch.equal(only_y, dY)
+        none, only_w = som.som_combine_grad(gd, Yd, slot_d, weight=wd, dY=False)
+        assert none is None and torch.equal(only_w, dweight)
+    if T * k:
+        assert som.som_dispatch(Xd, slot_d).shape == (T * k, D)
+
+
+def test_rows_that_are_no_numbers_stay_where_they_are(som):
+    """A row of NaN or infinities reaches its own places and results only; a pair without a place reads nothing."""
+    node = torch.tensor([[0, 1], [1, -1], [0, 1]], dtype=torch.int32)
+    _, _, slot = ref.group(node, 2)
+    X = torch.ones(3, 40)
+    X[1, 3], X[2, 5] = float("nan"), float("inf")
+    Y = som.som_dispatch(X.cuda(), slot.cuda(), out=torch.zeros(6, 40, device="cuda"))
+    assert torch.equal(torch.isnan(Y.cpu()).any(1), torch.tensor([False, False, False, True, False, False]))
+    poisoned = torch.full((6, 40), float("nan"))
+    poisoned[:5] = 1.0                                                     # the sixth place is nobody's
+    out = som.som_combine(poisoned.cuda(), slot.cuda())
+    assert torch.equal(out.cpu(), torch.tensor([2.0, 1.0, 2.0])[:, None].expand(3, 40))
+
+
+def test_slots_outside_the_places_are_not_followed(som):
+    slot = torch.tensor([[0, 99], [-7, 1], [2 ** 31 - 1, -2 ** 31]], dtype=torch.int32)
+    X, Y = torch.randn(3, 33).bfloat16(), torch.randn(4, 33).bfloat16()
+    out = torch.zeros(4, 33, dtype=torch.bfloat16)
+    ref.check(som.som_dispatch(X.cuda(), slot.cuda(), out=out.cuda()), *ref.dispatch(X, slot, None, out), "dispatch")
+    ref.check(som.som_combine(Y.cuda(), slot.cuda()), *ref.combine(Y, slot, None), "combine")
+    dY, dw = som.som_combine_grad(X.cuda(), Y.cuda(), slot.cuda(), dY=out.cuda())
+    want = ref.combine_grad(X, Y, slot, None, out)
+    ref.check(dY, want[0], want[1], "dY")
+    ref.check(dw, want[2], want[3], "dweight")
+
+
+def cut(gen, M, K, how):
+    """Offsets of K nodes over M rows."""
+    if how == "one":
+        counts = torch.zeros(K, dtype=torch.long)
+        counts[K // 2] = M
+    else:
+        share = torch.rand(K, generator=gen) ** (8 if how == "skew" else 1) + 1e-9
+        if K > 2:
+            share[torch.rand(K, generator=gen) < 0.2] = 0
+            share[0] += 1e-6
+        counts = torch.floor(share / share.sum() * M).long()
+        counts[int(counts.argmax())] += M - int(counts.sum())
+    if how == "tail":                               # rows behind the last node's
+        counts[int(counts.argmax())] -= min(int(counts.max()), 5)
+    return torch.cat([torch.zeros(1, dtype=torch.long), counts.cumsum(0)]).int()
+
+
+#           M, K, Din, Dout, extra, lead, how, act, bias, residual, pre
+PRODUCTS = [(1, 1, 1, 1, 0, 0, "whole", "none", False, False, False), (1, 4, 64, 64, 0, 0, "even", "silu", True, True, True),
+            (3, 5, 7, 5, 3, 1, "even", "gelu", True, False, True), (40, 8, 128, 96, 0, 0, "tail", "gelu_tanh", True, True, True),
+            (70, 3, 50, 16, 0, 0, "even", "none", True, False, False), (200, 37, 37, 24, 0, 0, "tail", "relu", True, True, False),
+            (130, 1, 100, 257, 0, 0, "whole", "silu", False, True, False), (300, 4, 264, 136, 8, 0, "skew", "gelu_tanh", True, False, True),
+            (257, 2, 513, 300, 1, 1, "even", "relu", False, False, True), (515, 3, 256, 512, 0, 0, "one", "gelu", True, True, True),
+            (64, 64, 512, 64, 0, 0, "even", "none", False, True, False), (16, 200, 72, 40, 0, 8, "even", "silu", True, False, False),
+            (1030, 2, 192, 320, 0, 0, "tail", "none", True, False, True), (900, 700, 16, 8, 0, 0, "skew", "relu", True, True, True),
+            (31, 1, 1024, 24, 0, 0, "whole", "gelu", True, True, True), (600, 1, 64, 1024, 64, 64, "whole", "gelu_tanh", True, True, True),
+            (2, 1, 4096, 130, 0, 0, "whole", "none", False, False, False), (5, 1, 33, 2050, 0, 0, "whole", "silu", True, False, True)]
+
+
+@pytest.mark.parametrize("dtype", ref.TYPES)
+@pytest.mark.parametrize("M, K, Din, Dout, extra, lead, how, act, bias, residual, pre", PRODUCTS)
+def test_product_and_gradient(som, M, K, Din, Dout, extra, lead, how, act, bias, residual, pre, dtype):
+    gen = torch.Generator().manual_seed(M + Din)
+    offsets = None if how == "whole" else cut(gen, M, K, how)
+    X, A = normal(gen, M, Din, dtype=dtype), normal(gen, K, Dout, Din, dtype=dtype, scale=Din ** -0.5)
+    if offsets is None:
+        A = A[0]
+    c = normal(gen, *A.shape[:-2], Dout, dtype=dtype) if bias else None
+    R = normal(gen, M, Dout, dtype=dtype) if residual else None
+    before, before_x = normal(gen, M, Dout, dtype=dtype), normal(gen, M, Din, dtype=dtype)
+    dev = lambda t: None if t is None else t.cuda()
+    Xd, Ad, offd = padded(X, extra, lead), A.cuda(), dev(offsets)
+    out, z = padded(before, extra, lead), padded(before, extra, 0) if pre else None
+    som.som_node_product(Xd, Ad, offsets=offd, bias=dev(c), activation=act, residual=None if R is None else padded(R, extra, lead), pre=z, out=out)
+    want, bound, wz, bz = ref.product(X, A, offsets, c, act, R, before, before)
+    ref.check(out, want, bound, "Y")
+    if pre:
+        ref.check(z, wz, bz, "pre")
+    dY, Z = normal(gen, M, Dout, dtype=dtype), normal(gen, M, Dout, dtype=dtype, scale=2.0)
+    dX = padded(before_x, extra, lead)
+    got = som.som_node_product_grad(padded(dY, extra, lead), Xd, Ad, offsets=offd, pre=padded(Z, extra, 0) if act != "none" else None, activation=act, dX=dX)
+    want = ref.product_grad(dY, X, A, offsets, Z, act, before_x)
+    for g, i, name in zip(got, (0, 2, 4), ("dX", "dA", "dbias")):
+        ref.check(g, want[i], want[i + 1], name)
+    # each alone, and again: the same bits
+    zd = padded(Z, 0, 0) if act != "none" else None
+    for which in range(3):
+        args = [False, False, False]
+        args[which] = padded(before_x, extra, lead) if which == 0 else None
+        alone = som.som_node_product_grad(padded(dY, 0, 0), Xd, Ad, offsets=offd, pre=zd, activation=act, dX=args[0], dA=args[1], dbias=args[2])
+        assert torch.equal(alone[which], got[which]) and [t is None for t in alone] == [i != which for i in range(3)]
+
+
+@pytest.mark.parametrize("dtype", ref.TYPES)
+def test_product_without_rows(som, dtype):
+    X, A = torch.empty(0, 24, dtype=dtype, device="cuda"), torch.randn(3, 8, 24, device="cuda").to(dtype)
+    offsets = torch.zeros(4, dtype=torch.int32, device="cuda")
+    assert som.som_node_product(X, A, offsets=offsets).shape == (0, 8)
+    dX, dA, dbias = som.som_node_product_grad(torch.empty(0, 8, dtype=dtype, device="cuda"), X, A, offsets=offsets)
+    assert dX.shape == (0, 24) and not dA.any() and not dbias.any() and dA.shape == A.shape and dbias.shape == (3, 8)
+
+
+@pytest.mark.parametrize("dtype", ref.TYPES)
+@pytest.mark.parametrize("Din, Dout", [(72, 40), (37, 21), (256, 256)])
+def test_rows_behind_a_group_do_not_reach_it(som, Din, Dout, dtype):
+    """NaN in one node's rows, and in rows that are no node's, stays out of every other node's results and gradients."""
+    gen = torch.Generator().manual_seed(3)
+    offsets = torch.tensor([0, 5, 5, 75, 80], dtype=torch.int32)
+    X, A, dY = normal(gen, 90, Din, dtype=dtype), normal(gen, 4, Dout, Din, dtype=dtype, scale=Din ** -0.5), normal(gen, 90, Dout, dtype=dtype)
+    X[75:], dY[75:] = float("nan"), float("nan")
+    A[3] = float("inf")
+    before, before_x = torch.zeros(90, Dout, dtype=dtype), torch.zeros(90, Din, dtype=dtype)
+    Y = som.som_node_product(X.cuda(), A.cuda(), offsets=offsets.cuda(), out=before.cuda()).cpu()
+    dX, dA, dbias = (t.cpu() for t in som.som_node_product_grad(dY.cuda(), X.cuda(), A.cuda(), offsets=offsets.cuda(), dX=before_x.cuda()))
+    live = torch.arange(90) < 75
+    want, bound, _, _ = ref.product(X[:75], A[:3], offsets[:4], None, "none", None, before[:75], before[:75])
+    ref.check(Y[live], want, bound, "Y")
+    assert torch.isnan(Y[75:80]).all() and not Y[80:].any() and not dX[80:].any()
+    grads = ref.product_grad(dY[:75], X[:75], A[:3], offsets[:4], None, "none", before_x[:75])
+    ref.check(dX[live], grads[0], grads[1], "dX")
+    ref.check(dA[:3], grads[2], grads[3], "dA")
+    ref.check(dbias[:3], grads[4], grads[5], "dbias")
+    assert torch.isnan(dA[3]).all() and torch.isnan(dbias[3]).all()
+
+
+def test_offsets_outside_the_rows_are_cut_off(som):
+    """Offsets beyond the rows, or falling ones: the rows that exist are taken, nothing beyond them."""
+    gen = torch.Generator().manual_seed(4)
+    X, A = normal(gen, 20, 24, dtype=torch.bfloat16), normal(gen, 3, 16, 24, dtype=torch.bfloat16)
+    before = torch.zeros(20, 16, dtype=torch.bfloat16)
+    Y = som.som_node_product(X.cuda(), A.cuda(), offsets=torch.tensor([-5, 8, 8, 1000], dtype=torch.int32).cuda(), out=before.cuda())
+    want, bound, _, _ = ref.product(X, A, torch.tensor([0, 8, 8, 20]), None, "none", None, before, before)
+    ref.check(Y, want, bound, "Y")
+    dX, dA, dbias = som.som_node_product_grad(before.cuda(), X.cuda(), A.cuda(), offsets=torch.tensor([9, 3, 99, 50], dtype=torch.int32).cuda())
+    assert not dA.any() and not dbias.any()
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh", "relu"])
+@pytest.mark.parametrize("dtype", ref.TYPES)
+def test_activations_over_their_whole_range(som, act, dtype):
+    """One feature, one matrix of one entry: the activation of every value from far left to far right, infinities and NaN among them."""
+    v = torch.cat([torch.linspace(-12, 12, 1501), torch.tensor([0.0, -0.0, 1e-30, -1e-30, 40, -40, 200, -200, 6e4, -6e4, math.inf, -math.inf, math.nan])])
+    X = v[:, None].to(dtype)
+    A = torch.ones(1, 1, dtype=dtype)
+    zero = torch.zeros_like(X)
+    Y = som.som_node_product(X.cuda(), A.cuda(), activation=act)
+    want, bound, _, _ = ref.product(X, A, None, None, act, None, zero, zero)
+    ref.check(Y, want, bound, "Y")
+    dX, _, _ = som.som_node_product_grad(torch.ones_like(X).cuda(), X.cuda(), A.cuda(), pre=X.cuda(), activation=act)
+    want = ref.product_grad(torch.ones_like(X), X, A, None, X, act, zero)
+    ref.check(dX, want[0], want[1], "dX")
+
+
+def test_a_training_step_of_local_models_on_a_map(som):
+    """As they are used together: units of a trained map and their neighbours route rows through two layers of local models,
+    then the whole way back; every stage against the reference on the stage's own inputs."""
+    from paper_2604_26555_amd.topology import lattice_distances
+    gen = torch.Generator().manual_seed(12)
+    T, D, H, O, K, k = 700, 50, 40, 6, 30, 3
+    X, W = normal(gen, T, D), normal(gen, K, D)
+    G = torch.from_numpy(lattice_distances(5, 6, "hex"))
+    Xd = X.cuda()
+    bmu, _, _ = som.som_bmu(Xd, W.cuda())
+    near = torch.sort(G, dim=1, stable=True).indices[:, :k].int()          # every node and its two nearest
+    node = near.cuda()[bmu.long()].contiguous()
+    node[::50] = -1
+    weight = torch.softmax(-G.cuda()[bmu.long()[:, None], node.long().clamp(min=0)], 1).contiguous()
+    A1, c1, A2, c2 = normal(gen, K, H, D, scale=D ** -0.5), normal(gen, K, H), normal(gen, K, O, H, scale=H ** -0.5), normal(gen, K, O)
+    target = normal(gen, T, O).cuda()
+    A1d, c1d, A2d, c2d = A1.cuda(), c1.cuda(), A2.cuda(), c2.cuda()
+
+    offsets, _, slot = som.som_group(node, K)
+    Xg = som.som_dispatch(Xd, slot, out=torch.zeros(T * k, D, device="cuda"))
+    pre = torch.zeros(T * k, H, device="cuda")
+    Hg = som.som_node_product(Xg, A1d, offsets=offsets, bias=c1d, activation="gelu_tanh", pre=pre, out=torch.zeros(T * k, H, device="cuda"))
+    Yg = som.som_node_product(Hg, A2d, offsets=offsets, bias=c2d, out=torch.zeros(T * k, O, device="cuda"))
+    out = som.som_combine(Yg, slot, weight=weight)
+    dout = out - target
+    dYg, dweight = som.som_combine_grad(dout, Yg, slot, weight=weight, dY=torch.zeros(T * k, O, device="cuda"))
+    dHg, dA2, dc2 = som.som_node_product_grad(dYg, Hg, A2d, offsets=offsets, dX=torch.zeros(T * k, H, device="cuda"))
+    dXg, dA1, dc1 = som.som_node_product_grad(dHg, Xg, A1d, offsets=offsets, pre=pre, activation="gelu_tanh", dX=torch.zeros(T * k, D, device="cuda"))
+    dX = som.som_combine(dXg, slot)
+    som.som_sync()
+
+    c = lambda t: t.cpu()
+    zero = lambda n: torch.zeros(T * k, n)
+    off, _, sl = ref.group(c(node), K)
+    assert torch.equal(c(offsets), off) and torch.equal(c(slot), sl) and int(off[-1]) == 3 * (T - 14)
+    ref.check(Xg, *ref.dispatch(X, sl, None, zero(D)), "rows")
+    y, b, z, zb = ref.product(c(Xg), A1, off, c1, "gelu_tanh", None, zero(H), zero(H))
+    ref.check(Hg, y, b, "hidden")
+    ref.check(pre, z, zb, "pre")
+    y, b, _, _ = ref.product(c(Hg), A2, off, c2, "none", None, zero(O), zero(O))
+    ref.check(Yg, y, b, "results")
+    ref.check(out, *ref.combine(c(Yg), sl, c(weight)), "out")
+    y, b, dw, dwb = ref.combine_grad(c(dout), c(Yg), sl, c(weight), zero(O))
+    ref.check(dYg, y, b, "dYg")
+    ref.check(dweight, dw, dwb, "dweight")
+    for got, want in (((dHg, dA2, dc2), ref.product_grad(c(dYg), c(Hg), A2, off, None, "none", zero(H))),
+                      ((dXg, dA1, dc1), ref.product_grad(c(dHg), c(Xg), A1, off, c(pre), "gelu_tanh", zero(D)))):
+        for g, i in zip(got, (0, 2, 4)):
+            ref.check(g, want[i], want[i + 1], "gradient")
+    ref.check(dX, *ref.combine(c(dXg), sl, None), "dX")
+
+
+def test_captured_and_replayed_on_changing_inputs(som):
+    """Group, dispatch, product and gradients in one graph, replayed on other rows with eager calls in between."""
+    gen = torch.Generator().manual_seed(7)
+    T, k, K, D, H = 300, 2, 11, 72, 40
+    X, node = torch.zeros(T, D, dtype=torch.bfloat16, device="cuda"), torch.zeros(T, k, dtype=torch.int32, device="cuda")
+    A = normal(gen, K, H, D, dtype=torch.bfloat16, scale=D ** -0.5).cuda()
+    dY = normal(gen, T * k, H, dtype=torch.bfloat16).cuda()
+    from paper_2604_26555_amd import Som
+    stream = torch.cuda.Stream()
+    mine = Som(0, stream)
+    z = lambda n: torch.zeros(T * k, n, dtype=torch.bfloat16, device="cuda")
+    bufs = dict(Xg=z(D), pre=z(H), Y=z(H), dX=z(D))
+
+    def step(s, b):
+        offsets, order, slot = s.som_group(node, K)
+        s.som_dispatch(X, slot, out=b["Xg"])
+        s.som_node_product(b["Xg"], A, offsets=offsets, activation="silu", pre=b["pre"], out=b["Y"])
+        _, dA, dbias = s.som_node_product_grad(dY, b["Xg"], A, offsets=offsets, pre=b["pre"], activation="silu", dX=b["dX"])
+        return [offsets, order, slot, b["Xg"], b["pre"], b["Y"], b["dX"], dA, dbias]
+
+    def fill(i):
+        g = torch.Generator().manual_seed(100 + i)
+        X.copy_(normal(g, T, D, dtype=torch.bfloat16))
+        node.copy_(draw_nodes(g, T, k, K, ("even", "holes", "one")[i % 3]))
+
+    fill(0)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        step(mine, bufs)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        outs = step(mine, bufs)
+    for i in range(4):
+        fill(i)
+        for b in bufs.values():
+            b.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = step(som, {n: torch.zeros_like(b) for n, b in bufs.items()})
+        torch.cuda.synchronize()
+        for a, b in zip(outs, eager):
+            assert torch.equal(a, b), f"replay {i}"
+    mine.close()
+
+
+def test_outputs_made_for_a_stream_of_their_own(som):
+    """A context on a stream other than the current one: its outputs' memory comes from that stream's pool."""
+    from paper_2604_26555_amd import Som
+    side = torch.cuda.Stream()
+    mine = Som(0, side)
+    X = torch.randn(2000, 256, device="cuda")
+    node = torch.randint(0, 16, (2000, 2), device="cuda", dtype=torch.int32)
+    torch.cuda.synchronize()
+    offsets, _, slot = mine.som_group(node, 16)
+    Y = mine.som_combine(mine.som_dispatch(X, slot), slot)
+    mine.som_sync()
+    assert torch.equal(Y, X + X) and int(offsets[-1]) == 4000
+    mine.close()
+
+
+def test_python_refusals(som):
+    X, A = torch.zeros(6, 8, device="cuda"), torch.zeros(2, 4, 8, device="cuda")
+    off, slot = torch.tensor([0, 3, 6], dtype=torch.int32, device="cuda"), torch.zeros(6, 1, dtype=torch.int32, device="cuda")
+    for error, f in [
+        (TypeError, lambda: som.som_group(slot.long(), 2)), (ValueError, lambda: som.som_group(slot.cpu(), 2)),
+        (ValueError, lambda: som.som_group(torch.zeros(4, 4, dtype=torch.int32, device="cuda").t()[:2], 2)),
+        (ValueError, lambda: som.som_group(slot, 2, offsets=off[:2])),
+        (TypeError, lambda: som.som_dispatch(X.double(), slot)), (ValueError, lambda: som.som_dispatch(X.t(), slot)),
+        (ValueError, lambda: som.som_dispatch(X[:5], slot)), (ValueError, lambda: som.som_dispatch(X, slot, weight=torch.zeros(6, 2, device="cuda"))),
+        (TypeError, lambda: som.som_dispatch(X, slot, out=X.half())), (ValueError, lambda: som.som_dispatch(X, slot, out=X[:, :7])),
+        (ValueError, lambda: som.som_combine(X, slot, out=torch.zeros(5, 8, device="cuda"))), (TypeError, lambda: som.som_combine(X, slot.float())),
+        (ValueError, lambda: som.som_combine_grad(X[:5], X, slot)), (TypeError, lambda: som.som_combine_grad(X.half(), X, slot)),
+        (ValueError, lambda: som.som_node_product(X, A)), (ValueError, lambda: som.som_node_product(X, A, offsets=off[:2])),
+        (ValueError, lambda: som.som_node_product(X[:, :7], A, offsets=off)), (TypeError, lambda: som.som_node_product(X, A.half(), offsets=off)),
+        (ValueError, lambda: som.som_node_product(X, A, offsets=off, bias=torch.zeros(2, 3, device="cuda"))),
+        (ValueError, lambda: som.som_node_product(X, A, offsets=off, residual=torch.zeros(6, 5, device="cuda"))),
+        (ValueError, lambda: som.som_node_product(X, A.transpose(1, 2), offsets=off)), (KeyError, lambda: som.som_node_product(X, A, offsets=off, activation="x")),
+        (ValueError, lambda: som.som_node_product_grad(X, X, A, offsets=off)),
+        (Exception, lambda: som.som_node_product_grad(torch.zeros(6, 4, device="cuda"), X, A, offsets=off, activation="relu")),
+    ]:
+        with pytest.raises(error):
+            f()

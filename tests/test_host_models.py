@@ -1,0 +1,182 @@
+"""Local models on a machine without a GPU: what the entry points refuse, and what the reference of their GPU tests is."""
+import ctypes as C
+
+import pytest
+import torch
+
+import models_reference as ref
+import stub_library
+from paper_2604_26555_amd import SOM_EINVAL, SOM_OK
+
+i32, i64 = C.c_int32, C.c_int64
+
+
+@pytest.fixture(scope="module")
+def stub(tmp_path_factory):
+    return stub_library.link(str(tmp_path_factory.mktemp("stub")))
+
+
+@pytest.fixture
+def ctx(stub):
+    c = stub_library.StubContext(stub)
+    yield c
+    c.close()
+
+
+GROUP = dict(node="p", T=7, k=2, K=5, offsets="p", order="p", slot="p")
+DISPATCH = dict(type=1, X="p", T=7, D=16, ldx=16, slot="p", k=2, weight="p", Y="p", M=14, ldy=16)
+COMBINE = dict(type=1, Y="p", M=14, D=16, ldy=16, slot="p", T=7, k=2, weight="p", out="p", ldo=16)
+COMBINE_GRAD = dict(type=2, dout="p", T=7, D=16, lddo=16, Y="p", M=14, ldy=16, slot="p", k=2, weight="p", dY="p", lddy=16, dweight="p")
+PRODUCT = dict(type=0, X="p", M=14, Din=16, ldx=16, offsets="p", K=5, A="p", Dout=8, bias="p", act=2, residual="p", ldr=8, pre="p", ldpre=8, Y="p", ldy=8)
+PRODUCT_GRAD = dict(type=0, dY="p", M=14, Dout=8, lddy=8, X="p", Din=16, ldx=16, offsets="p", K=5, A="p", pre="p", ldpre=8, act=2, dX="p", lddx=16,
+                    dA="p", dbias="p")
+CALLS = dict(som_group=GROUP, som_dispatch=DISPATCH, som_combine=COMBINE, som_combine_grad=COMBINE_GRAD, som_node_product=PRODUCT,
+             som_node_product_grad=PRODUCT_GRAD)
+WIDE = {"T", "M", "ldx", "ldy", "ldo", "lddo", "lddy", "lddx", "ldr", "ldpre"}
+
+
+def call(ctx, name, **changes):
+    args = []
+    for key, v in {**CALLS[name], **changes}.items():
+        if v == "p":
+            args.append(ctx._p)
+        elif v == "odd":
+            args.append(C.c_void_p(ctx._p.value + 1))
+        elif v is None:
+            args.append(C.c_void_p(None))
+        else:
+            args.append(i64(v) if key in WIDE else i32(v))
+    return ctx._run(getattr(ctx.lib, name), *args)
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_plain_calls_launch(ctx, name):
+    rc, kernels = call(ctx, name)
+    assert rc == SOM_OK and kernels, ctx.error()
+
+
+REFUSED = [
+    ("som_group", dict(node=None), "node"), ("som_group", dict(offsets=None), "offsets"), ("som_group", dict(T=-1), "negative"),
+    ("som_group", dict(k=0), "k=0"), ("som_group", dict(K=0), "K (0)"), ("som_group", dict(K=32769), "32768"),
+    ("som_group", dict(T=2 ** 30, k=2), "2^31-1"), ("som_group", dict(T=2 ** 62, k=4), "2^31-1"), ("som_group", dict(node="odd"), "aligned"),
+    ("som_dispatch", dict(type=3), "type"), ("som_dispatch", dict(X=None), "X"), ("som_dispatch", dict(Y=None), "Y"),
+    ("som_dispatch", dict(slot=None), "slot"), ("som_dispatch", dict(D=0), "width"), ("som_dispatch", dict(ldx=15), "X: leading"),
+    ("som_dispatch", dict(ldy=15), "Y: leading"), ("som_dispatch", dict(M=-1), "negative"), ("som_dispatch", dict(M=2 ** 31), "2^31-1"),
+    ("som_dispatch", dict(D=2 ** 20 + 1, ldx=2 ** 20 + 1, ldy=2 ** 20 + 1), "width"), ("som_dispatch", dict(ldx=2 ** 21 + 1), "above"),
+    ("som_dispatch", dict(X="odd"), "aligned"),
+    ("som_combine", dict(out=None), "out"), ("som_combine", dict(Y=None), "Y"), ("som_combine", dict(ldo=1), "out: leading"),
+    ("som_combine", dict(type=-1), "type"), ("som_combine", dict(k=-3), "k=-3"),
+    ("som_combine_grad", dict(dY=None, dweight=None), "neither"), ("som_combine_grad", dict(dout=None), "dout"),
+    ("som_combine_grad", dict(Y=None), "Y"), ("som_combine_grad", dict(lddy=7), "dY: leading"), ("som_combine_grad", dict(lddo=7), "dout: leading"),
+    ("som_node_product", dict(X=None), "X"), ("som_node_product", dict(A=None), "A"), ("som_node_product", dict(Y=None), "Y"),
+    ("som_node_product", dict(offsets=None), "one node"), ("som_node_product", dict(act=5), "activation"), ("som_node_product", dict(act=-1), "activation"),
+    ("som_node_product", dict(K=0), "K (0)"), ("som_node_product", dict(Dout=0), "width"), ("som_node_product", dict(ldr=7), "residual: leading"),
+    ("som_node_product", dict(ldpre=7), "pre: leading"), ("som_node_product", dict(ldy=7), "Y: leading"),
+    ("som_node_product_grad", dict(dX=None, dA=None, dbias=None), "none of"), ("som_node_product_grad", dict(pre=None), "pre"),
+    ("som_node_product_grad", dict(dY=None), "dY"), ("som_node_product_grad", dict(X=None), "X"), ("som_node_product_grad", dict(A=None), "A"),
+    ("som_node_product_grad", dict(lddx=15), "dX: leading"), ("som_node_product_grad", dict(offsets=None), "one node"),
+]
+
+
+@pytest.mark.parametrize("name, changes, says", REFUSED)
+def test_refusals_name_their_reason_and_launch_nothing(ctx, name, changes, says):
+    rc, kernels = call(ctx, name, **changes)
+    assert rc == SOM_EINVAL and kernels == [] and says in ctx.error(), (rc, kernels, ctx.error())
+
+
+def test_optional_arguments(ctx):
+    assert call(ctx, "som_group", order=None, slot=None)[0] == SOM_OK
+    assert call(ctx, "som_dispatch", weight=None)[0] == SOM_OK
+    assert call(ctx, "som_combine_grad", Y=None, dweight=None)[0] == SOM_OK               # Y serves the weights' gradient only
+    assert call(ctx, "som_node_product", bias=None, residual=None, pre=None)[0] == SOM_OK
+    assert call(ctx, "som_node_product", offsets=None, K=1)[0] == SOM_OK
+    assert call(ctx, "som_node_product_grad", pre=None, act=0)[0] == SOM_OK
+    assert call(ctx, "som_node_product_grad", A=None, dX=None)[0] == SOM_OK
+    assert call(ctx, "som_node_product_grad", X=None, dA=None)[0] == SOM_OK
+
+
+def test_calls_on_nothing(ctx):
+    """No rows: nothing is launched but what clears the outputs that have a value of their own."""
+    rc, kernels = call(ctx, "som_group", T=0, node=None, order=None, slot=None)
+    assert rc == SOM_OK and len(kernels) == 1
+    assert call(ctx, "som_dispatch", T=0, X=None, slot=None, weight=None) == (SOM_OK, [])
+    assert call(ctx, "som_combine", T=0, out=None, slot=None) == (SOM_OK, [])
+    assert call(ctx, "som_combine", M=0, Y=None)[0] == SOM_OK                               # rows of zeros
+    assert call(ctx, "som_node_product", M=0, X=None, Y=None) == (SOM_OK, [])
+    rc, kernels = call(ctx, "som_node_product_grad", M=0, X=None, dY=None, pre=None, dX=None)
+    assert rc == SOM_OK and kernels                                                        # zeros for dA and dbias
+
+
+def test_null_context(stub):
+    lib = C.CDLL(stub)
+    for name, call_args in CALLS.items():
+        assert getattr(lib, name)(None, *[C.c_void_p(None) if v == "p" else (i64(v) if key in WIDE else i32(v)) for key, v in call_args.items()]) == SOM_EINVAL
+
+
+def test_without_memory_for_the_workspace(ctx):
+    ctx.limit(16)
+    rc, kernels = call(ctx, "som_group")
+    assert rc == -2 and kernels == [] and "workspace" in ctx.error()
+    rc, kernels = call(ctx, "som_node_product_grad")
+    assert rc == -2 and kernels == []
+    ctx.limit()
+    assert call(ctx, "som_group")[0] == SOM_OK
+
+
+def test_a_failed_launch_is_reported(ctx):
+    for name in CALLS:
+        rc, kernels = call(ctx, name)
+        ctx.fail(kernels[-1].split("<")[0])
+        rc, _ = call(ctx, name)
+        assert rc == -3 and "launch" in ctx.error(), name
+        ctx.fail()
+
+
+def test_reference_group_by_hand():
+    offsets, order, slot = ref.group(torch.tensor([[2, 0], [0, -1], [7, 2]], dtype=torch.int32), 3)
+    assert offsets.tolist() == [0, 2, 2, 4] and order.tolist() == [1, 2, 0, 5, -1, -1] and slot.tolist() == [[2, 0], [1, -1], [-1, 3]]
+
+
+@pytest.mark.parametrize("act", ref.ACTIVATIONS)
+def test_reference_gradients_against_autograd_and_differences(act):
+    """The reference's formulas: sorted rows, products and the way back, against torch's derivatives and central differences."""
+    gen = torch.Generator().manual_seed(5)
+    node = torch.randint(-1, 4, (9, 2), generator=gen).int()
+    offsets, _, slot = ref.group(node, 4)
+    w = torch.rand(9, 2, generator=gen, dtype=torch.float64)
+    X, A, c, g = (torch.randn(*s, generator=gen, dtype=torch.float64) for s in ((9, 5), (4, 3, 5), (4, 3), (9, 3)))
+    off = offsets.tolist()
+
+    def loss(X, A, c, w):
+        total = 0.0
+        for t in range(9):
+            for j in range(2):
+                if slot[t, j] >= 0:
+                    e = int(node[t, j])
+                    total = total + w[t, j] * (g[t] * ref.activation(A[e] @ X[t] + c[e], act)[0]).sum()
+        return total
+
+    places = torch.zeros(18, 5, dtype=torch.float64)
+    Xg = ref.dispatch(X, slot, None, places)[0]
+    empty = torch.zeros(18, 3, dtype=torch.float64)
+    Y, _, pre, _ = ref.product(Xg, A, offsets, c, act, None, empty, empty)
+    dY, _, dw, _ = ref.combine_grad(g, Y, slot, w, empty)
+    dXg, _, dA, _, dc, _ = ref.product_grad(dY, Xg, A, offsets, pre, act, places)
+    dX = ref.combine(dXg, slot, None)[0]
+    leaves = [v.clone().requires_grad_() for v in (X, A, c, w)]
+    auto = torch.autograd.grad(loss(*leaves), leaves)
+    # float64 throughout, but for dz, whose bound and not value is rounded: agreement to 2^-40 of the largest entry
+    for got, want in zip((dX, dA, dc, dw), auto):
+        assert (got - want).abs().max() <= 2.0 ** -40 * want.abs().max().clamp(min=1)
+    step = 2.0 ** -13
+    for got, i in zip((dX, dA, dc, dw), range(4)):
+        args = [X, A, c, w]
+        d = torch.randn(args[i].shape, generator=gen, dtype=torch.float64)
+        up, down = list(args), list(args)
+        up[i], down[i] = args[i] + step * d, args[i] - step * d
+        slope = (loss(*up) - loss(*down)) / (2 * step)
+        if act == "relu":
+            continue                                     # (not differentiable where a step crosses zero)
+        # the third derivative of a term is below 4 |d . A|^3 |g w|: of some forty terms of size 5 a thousandth of 2^-6 remains
+        assert abs(float((got * d).sum() - slope)) <= 2.0 ** -12 * (1 + abs(float(slope)))
+    assert off[-1] == int((slot >= 0).sum())
