@@ -235,6 +235,232 @@ __global__ void __launch_bounds__(256) product_any_kernel(ProductArgs<T> a)
     }
 }
 
+// ---------------------------------------------------------------------------------------------------------------- wide tiles
+// 16-bit rows whose addresses, widths and leading dimensions are multiples of sixteen bytes.
+
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) char lds_char;
+
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(const lds_char*)p; }
+
+// 64 lanes' sixteen bytes from `offset` behind a buffer's base to LDS at `lds`, in lane order; offsets beyond the buffer's length
+// bring zeros.  (Waited for by vmcnt, in the order of issue.)
+__device__ __forceinline__ void buffer_to_lds(uint32_t lds, uint32_t offset, v4i buffer)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(buffer) : "memory", "m0");
+}
+
+__device__ __forceinline__ v4i buffer_of(const void* base, uint32_t bytes)
+{
+    const uint64_t a = (uint64_t)base;
+    v4i r;
+    r[0] = __builtin_amdgcn_readfirstlane((int)(uint32_t)a);
+    r[1] = __builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32) & 0xffff);
+    r[2] = __builtin_amdgcn_readfirstlane((int)bytes);
+    r[3] = 0x00020000;
+    return r;
+}
+
+constexpr uint32_t kNowhere = 0x80000000u;     // an offset behind every buffer
+
+// One operand of a tile: R rows (or, TR, columns) of the product by 64 of the contraction, 128 R bytes of LDS a stage.
+//   plain: memory holds R rows of `depth` values; LDS rows of 128 bytes, whose eight sixteen-byte chunks are exchanged by row & 7, so
+//          that 32 lanes that read one chunk of 32 rows meet all banks
+//   TR:    memory holds `depth` rows of R values; LDS rows of 2 R bytes, 64-byte pieces exchanged by row & 3: the transposing read
+//          of a half wavefront takes such a piece of four rows
+template <class T, int R, int WAVES, bool TR>
+struct Operand {
+    static constexpr int kBytes = R * 128, kLoads = kBytes / 1024 / WAVES;     // instructions of a wavefront a stage
+    static constexpr int kChunks = TR ? R / 8 : 8, kRowsAtOnce = 64 / kChunks; // LDS rows that an instruction fills
+    const T* base;             // the tile's first value
+    int64_t depth;             // of the contraction
+    uint32_t rows;             // plain: rows that exist, counted from base
+    uint32_t width;            // TR: values that exist in a row, counted from base
+    uint32_t ld;               // bytes
+    uint32_t offset[kLoads];
+    int chunk;                 // plain: which chunk this lane brings
+
+    __device__ __forceinline__ void init(const T* b, int64_t d, int64_t exist, int64_t stride, int wave, int lane)
+    {
+        base = b;
+        depth = d;
+        rows = width = (uint32_t)(exist < R ? exist : R);
+        ld = (uint32_t)(stride * 2);
+        const int c = lane % kChunks, r0 = wave * kLoads * kRowsAtOnce + lane / kChunks;
+        chunk = c ^ (lane / 8);
+#pragma unroll
+        for (int q = 0; q < kLoads; ++q) {
+            const int r = r0 + q * kRowsAtOnce;
+            if (TR) {
+                const uint32_t from = (uint32_t)(c ^ ((r & 3) << 2)) * 8;
+                offset[q] = from < width ? (uint32_t)r * ld + from * 2 : kNowhere;
+            } else {
+                offset[q] = (uint32_t)r * ld + (uint32_t)chunk * 16;
+            }
+        }
+    }
+    // the stage that starts at k0 (< depth) of the contraction
+    __device__ __forceinline__ void fetch(uint32_t lds, int64_t k0, int wave)
+    {
+        const int64_t left = depth - k0;
+        const uint32_t to = lds + (uint32_t)wave * kLoads * 1024;
+        if (TR) {
+            const uint32_t have = (uint32_t)(left < 64 ? left : 64);
+            const v4i buffer = buffer_of(base + k0 * (int64_t)(ld / 2), (have - 1) * ld + width * 2);
+#pragma unroll
+            for (int q = 0; q < kLoads; ++q) buffer_to_lds(to + q * 1024, offset[q], buffer);
+        } else {
+            const v4i buffer = buffer_of(base + k0, (rows - 1) * ld + (uint32_t)left * 2);
+            const bool past = chunk * 8 >= left;              // (left is a multiple of eight)
+#pragma unroll
+            for (int q = 0; q < kLoads; ++q) buffer_to_lds(to + q * 1024, past ? kNowhere : offset[q], buffer);
+        }
+    }
+};
+
+// 32 rows by 16 of the contraction as the matrix pipe takes them: lane l holds row l % 32, values 8 (l / 32) .. + 7.
+template <class T, int R, bool TR>
+__device__ __forceinline__ typename Half8<T>::type fragment(const char* stage, int r0, int k, int lane)
+{
+    union {
+        typename Half8<T>::type v;
+        s16x4 s[2];
+    } f;
+    if constexpr (!TR) {
+        const int r = r0 + (lane & 31), c = (k / 8 + (lane >> 5)) ^ (r & 7);
+        f.v = *reinterpret_cast<const typename Half8<T>::type*>(stage + r * 128 + c * 16);
+    } else {
+        // Sixteen lanes exchange a block of four rows and sixteen columns: lane 4 j + q brings columns 4 q .. + 3 of row j, lane i gets
+        // column i of all four.
+        typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+        const int row = k + 8 * (lane >> 5) + ((lane & 15) >> 2), col = r0 + (lane & 16) + 4 * (lane & 3);
+        const char* p = stage + row * (2 * R) + (((col >> 3) ^ ((row & 3) << 2)) << 4) + (col & 7) * 2;
+        f.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(s16x4*)p);
+        f.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(s16x4*)(p + 4 * (2 * R)));
+    }
+    return f.v;
+}
+
+template <int N>
+__device__ __forceinline__ void stage_ready()
+{
+    // this wavefront's loads up to N outstanding ones and its reads of the stage before are done; then everyone's are
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+template <class T, Form F, int BM, int BN, int WM, int WN, int STAGES>
+__global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64) product_tile_kernel(ProductArgs<T> a, int xtiles)
+{
+    constexpr int WAVES = (BM / WM) * (BN / WN), THREADS = WAVES * 64;
+    constexpr bool TP = F == kOuterSums, TQ = F != kRowsTimesA;
+    typedef Operand<T, BM, WAVES, TP> OpP;
+    typedef Operand<T, BN, WAVES, TQ> OpQ;
+    constexpr int kStage = OpP::kBytes + OpQ::kBytes, kLoads = OpP::kLoads + OpQ::kLoads;
+    extern __shared__ __align__(1024) char tile_lds[];
+    typedef typename Half8<T>::type half8;
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN) * WN;
+    const int Nn = F == kRowsTimesA ? a.dout : a.din;
+    int e;
+    int64_t first, end, m0 = 0;
+    const int nt = blockIdx.x % xtiles, mt = blockIdx.x / xtiles;
+    const int n0 = nt * BN;
+    if (F == kOuterSums) {
+        const int ytiles = (a.dout + BM - 1) / BM;
+        e = mt / ytiles;
+        m0 = (int64_t)(mt % ytiles) * BM;
+        group_rows(a.offsets, e, a.rows, first, end);
+    } else {
+        if (!find_tile<BM, THREADS>(a.offsets, a.K, a.rows, mt, e, first, end)) return;
+    }
+    OpP P;
+    OpQ Q;
+    const int64_t depth = F == kRowsTimesA ? a.din : F == kRowsTimesAt ? a.dout : end - first;
+    if (F == kOuterSums) {
+        P.init(a.P + first * a.ldp + m0, depth, a.dout - m0, a.ldp, wave, lane);
+        Q.init(a.Q + first * a.ldq + n0, depth, a.din - n0, a.ldq, wave, lane);
+    } else {
+        P.init(a.P + first * a.ldp, depth, end - first, a.ldp, wave, lane);
+        const T* A = a.Q + (int64_t)e * a.dout * a.din;
+        Q.init(F == kRowsTimesA ? A + (int64_t)n0 * a.din : A + n0, depth, Nn - n0, a.din, wave, lane);
+    }
+    f32x16 acc[WM / 32][WN / 32] = {};
+    const int steps = (int)((depth + 63) / 64);
+    const uint32_t lds = lds_address(tile_lds);
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s) {
+        if (s < steps) {
+            P.fetch(lds + s * kStage, (int64_t)s * 64, wave);
+            Q.fetch(lds + s * kStage + OpP::kBytes, (int64_t)s * 64, wave);
+        }
+    }
+    int slot = 0, ahead = STAGES - 1;
+    for (int i = 0; i < steps; ++i) {
+        if (i + STAGES - 1 <= steps) stage_ready<(STAGES - 2) * kLoads>();
+        else stage_ready<0>();
+        if (i + STAGES - 1 < steps) {
+            const int64_t k0 = (int64_t)(i + STAGES - 1) * 64;
+            P.fetch(lds + ahead * kStage, k0, wave);
+            Q.fetch(lds + ahead * kStage + OpP::kBytes, k0, wave);
+        }
+        const char* stage = tile_lds + slot * kStage;
+#pragma unroll
+        for (int k = 0; k < 64; k += 16) {
+            half8 p[WM / 32], q[WN / 32];
+#pragma unroll
+            for (int u = 0; u < WM / 32; ++u) p[u] = fragment<T, BM, TP>(stage, wm + 32 * u, k, lane);
+#pragma unroll
+            for (int u = 0; u < WN / 32; ++u) q[u] = fragment<T, BN, TQ>(stage + OpP::kBytes, wn + 32 * u, k, lane);
+#pragma unroll
+            for (int u = 0; u < WM / 32; ++u)
+#pragma unroll
+                for (int v = 0; v < WN / 32; ++v) acc[u][v] = mfma(q[v], p[u], acc[u][v]);
+        }
+        slot = slot + 1 == STAGES ? 0 : slot + 1;
+        ahead = ahead + 1 == STAGES ? 0 : ahead + 1;
+    }
+    // a lane holds row wm + 32 u + lane % 32 of the tile, four consecutive columns at a time
+    union Four {
+        uint2 w;
+        T e[4];
+    };
+#pragma unroll
+    for (int u = 0; u < WM / 32; ++u) {
+        const int m = wm + 32 * u + (lane & 31);
+        const int64_t row = F == kOuterSums ? m0 + m : first + m;
+        if (row >= (F == kOuterSums ? a.dout : end)) continue;
+        T* out = F == kOuterSums ? a.out + ((int64_t)e * a.dout + row) * a.din : a.out + row * a.ldo;
+#pragma unroll
+        for (int v = 0; v < WN / 32; ++v) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int n = n0 + wn + 32 * v + 8 * g + 4 * (lane >> 5);
+                if (n >= Nn) continue;
+                Four y, z, r, c;
+                if (F == kRowsTimesA) {
+                    if (a.bias) c.w = *reinterpret_cast<const uint2*>(a.bias + (int64_t)e * a.dout + n);
+                    if (a.residual) r.w = *reinterpret_cast<const uint2*>(a.residual + row * a.ldr + n);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float x = acc[u][v][4 * g + j];
+                    if (F == kRowsTimesA) {
+                        if (a.bias) x += (float)c.e[j];
+                        z.e[j] = (T)x;
+                        x = activate(x, a.act);
+                        if (a.residual) x += (float)r.e[j];
+                    }
+                    y.e[j] = (T)x;
+                }
+                if (F == kRowsTimesA && a.pre) *reinterpret_cast<uint2*>(a.pre + row * a.ldpre + n) = z.w;
+                *reinterpret_cast<uint2*>(out + n) = y.w;
+            }
+        }
+    }
+}
+
 // dz = dy act'(z), dense
 template <class T>
 __global__ void __launch_bounds__(256) slope_kernel(const T* __restrict__ dY, int64_t lddy, const T* __restrict__ pre, int64_t ldpre, int64_t rows,
@@ -271,9 +497,41 @@ static int64_t most_tiles(int64_t rows, int32_t K, const int32_t* offsets, int b
     return offsets ? full + (K < rows ? K : rows) : full;
 }
 
+static bool sixteen(const void* p) { return (uintptr_t)p % 16 == 0; }
+
+// What the wide tiles ask of a call: every row of every matrix starts at a multiple of sixteen bytes and has whole chunks of them.
+template <class T>
+static bool product_aligned(const ProductArgs<T>& a)
+{
+    return sizeof(T) == 2 && a.din % 8 == 0 && a.dout % 8 == 0 && a.ldp % 8 == 0 && a.ldq % 8 == 0 && a.ldo % 8 == 0 && a.ldr % 8 == 0 &&
+           a.ldpre % 8 == 0 && sixteen(a.P) && sixteen(a.Q) && sixteen(a.out) && sixteen(a.bias) && sixteen(a.residual) && sixteen(a.pre);
+}
+
+template <class T, Form F, int BM, int BN, int WM, int WN, int STAGES>
+static int product_tile_launch(som_ctx* ctx, const ProductArgs<T>& a, const char* what)
+{
+    constexpr int lds = STAGES * (BM + BN) * 128;
+    static bool attr_set_dev[kMaxDevices] = {};
+    bool& attr_set = attr_set_dev[ctx->device];
+    auto kern = product_tile_kernel<T, F, BM, BN, WM, WN, STAGES>;
+    if (!attr_set) {
+        if (int rc = check_hip(ctx, hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds),
+                               "raising the dynamic LDS limit"))
+            return rc;
+        attr_set = true;
+    }
+    const int xtiles = ((F == kRowsTimesA ? a.dout : a.din) + BN - 1) / BN;
+    const int64_t ytiles = F == kOuterSums ? (int64_t)a.K * ((a.dout + BM - 1) / BM) : most_tiles(a.rows, a.K, a.offsets, BM);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(xtiles * ytiles)), dim3((BM / WM) * (BN / WN) * 64), lds, ctx->stream, a, xtiles);
+    return check_hip(ctx, hipGetLastError(), what);
+}
+
 template <class T, Form F>
 static int product_launch(som_ctx* ctx, const ProductArgs<T>& a, const char* what)
 {
+    if constexpr (sizeof(T) == 2) {
+        if (product_aligned(a)) return product_tile_launch<T, F, 256, 256, 128, 64, 2>(ctx, a, what);
+    }
     const unsigned nx = (unsigned)(((F == kRowsTimesA ? a.dout : a.din) + 63) / 64);
     dim3 grid;
     if (F == kOuterSums) {
