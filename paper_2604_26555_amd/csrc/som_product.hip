@@ -41,38 +41,68 @@ struct ProductArgs {
 };
 
 // Where a factor has reached its limit the product with z is formed from the limit, so that infinities give what the function
-// tends to.  The error function's complement keeps the small values of the left tail to their last places.
+// tends to.
+//   float32 rows: the error function's complement keeps the small values of the left tail to their last places;
+//   16-bit rows: exponentials through the base-2 instruction (its argument's rounding is 2^-24 of the exponent, which the falling
+//   exponential outweighs), reciprocals to one unit, and the error function by Abramowitz and Stegun 7.1.26 (1.5e-7 at most): all of them
+//   some 2^-20 of |z| where the result is rounded by 2^-12 or 2^-9.
+template <bool EXACT>
+struct Math {
+    static __device__ __forceinline__ float exponential(float x) { return EXACT ? expf(x) : __builtin_amdgcn_exp2f(1.44269504f * x); }
+    static __device__ __forceinline__ float reciprocal(float x) { return EXACT ? 1.0f / x : __builtin_amdgcn_rcpf(x); }
+    // (1 + erf(z / sqrt 2)) / 2 for |z| <= 30; bell = exp(-z^2 / 2)
+    static __device__ __forceinline__ float gauss(float z, float bell)
+    {
+        if (EXACT) return 0.5f * erfcf(-0.70710678f * z);
+        const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.0f));
+        const float tail = 0.5f * bell * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+        return z > 0.0f ? 1.0f - tail : tail;
+    }
+    // (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2
+    static __device__ __forceinline__ float gate(float z)
+    {
+        return reciprocal(1.0f + exponential(-1.59576912f * z * fmaf(0.044715f, z * z, 1.0f)));
+    }
+
+    static __device__ __forceinline__ float activate(float z, int act)
+    {
+        switch (act) {
+        case SOM_ACT_RELU: return z < 0.0f ? 0.0f : z;                   // (a NaN stays one)
+        case SOM_ACT_SILU: return z < -110.0f ? 0.0f : z * reciprocal(1.0f + exponential(-z));
+        case SOM_ACT_GELU: return z < -30.0f ? 0.0f : z > 30.0f ? z : z * gauss(z, EXACT ? 0.0f : exponential(-0.5f * z * z));
+        case SOM_ACT_GELU_TANH: return z < -30.0f ? 0.0f : z > 30.0f ? z : z * gate(z);
+        }
+        return z;
+    }
+
+    static __device__ __forceinline__ float slope(float z, int act)
+    {
+        switch (act) {
+        case SOM_ACT_RELU: return z > 0.0f ? 1.0f : z == z ? 0.0f : z;
+        case SOM_ACT_SILU: {
+            if (fabsf(z) > 110.0f) return z > 0.0f ? 1.0f : 0.0f;
+            const float g = reciprocal(1.0f + exponential(-z));
+            return g * fmaf(z, 1.0f - g, 1.0f);
+        }
+        case SOM_ACT_GELU: {
+            if (fabsf(z) > 30.0f) return z > 0.0f ? 1.0f : 0.0f;
+            const float bell = exponential(-0.5f * z * z);
+            return fmaf(0.39894228f * z, bell, gauss(z, bell));
+        }
+        case SOM_ACT_GELU_TANH: {
+            if (fabsf(z) > 30.0f) return z > 0.0f ? 1.0f : 0.0f;
+            const float g = gate(z);
+            return g * fmaf(z * (1.0f - g) * 1.59576912f, fmaf(0.134145f, z * z, 1.0f), 1.0f);
+        }
+        }
+        return 1.0f;
+    }
+};
+
+template <class T>
 __device__ __forceinline__ float activate(float z, int act)
 {
-    switch (act) {
-    case SOM_ACT_RELU: return z < 0.0f ? 0.0f : z;                       // (a NaN stays one)
-    case SOM_ACT_SILU: return z < -110.0f ? 0.0f : z / (1.0f + expf(-z));
-    case SOM_ACT_GELU: return z < -30.0f ? 0.0f : 0.5f * z * erfcf(-0.70710678f * z);
-    case SOM_ACT_GELU_TANH:                                             // (1 + tanh u) / 2 = 1 / (1 + exp(-2 u))
-        return z < -30.0f ? 0.0f : z > 30.0f ? z : z / (1.0f + expf(-1.59576912f * (z + 0.044715f * z * z * z)));
-    }
-    return z;
-}
-
-__device__ __forceinline__ float slope(float z, int act)
-{
-    switch (act) {
-    case SOM_ACT_RELU: return z > 0.0f ? 1.0f : z == z ? 0.0f : z;
-    case SOM_ACT_SILU: {
-        if (fabsf(z) > 110.0f) return z > 0.0f ? 1.0f : 0.0f;
-        const float g = 1.0f / (1.0f + expf(-z));
-        return g * (1.0f + z * (1.0f - g));
-    }
-    case SOM_ACT_GELU:
-        if (fabsf(z) > 30.0f) return z > 0.0f ? 1.0f : 0.0f;
-        return 0.5f * erfcf(-0.70710678f * z) + z * expf(-0.5f * z * z) * 0.39894228f;
-    case SOM_ACT_GELU_TANH: {
-        if (fabsf(z) > 30.0f) return z > 0.0f ? 1.0f : 0.0f;
-        const float g = 1.0f / (1.0f + expf(-1.59576912f * (z + 0.044715f * z * z * z)));
-        return g * (1.0f + z * (1.0f - g) * 1.59576912f * (1.0f + 0.134145f * z * z));
-    }
-    }
-    return 1.0f;
+    return Math<sizeof(T) == 4>::activate(z, act);
 }
 
 // Rows [lo, hi) of group e, inside [0, rows) whatever the offsets hold.
@@ -228,7 +258,7 @@ __global__ void __launch_bounds__(256) product_any_kernel(ProductArgs<T> a)
         if (F == kRowsTimesA) {
             z += c;
             if (a.pre) a.pre[s * a.ldpre + n] = (T)z;
-            z = activate(z, a.act);
+            z = activate<T>(z, a.act);
             if (a.residual) z += (float)a.residual[s * a.ldr + n];
         }
         a.out[s * a.ldo + n] = (T)z;
@@ -264,15 +294,15 @@ __device__ __forceinline__ v4i buffer_of(const void* base, uint32_t bytes)
 
 constexpr uint32_t kNowhere = 0x80000000u;     // an offset behind every buffer
 
-// One operand of a tile: R rows (or, TR, columns) of the product by 64 of the contraction, 128 R bytes of LDS a stage.
-//   plain: memory holds R rows of `depth` values; LDS rows of 128 bytes, whose eight sixteen-byte chunks are exchanged by row & 7, so
-//          that 32 lanes that read one chunk of 32 rows meet all banks
+// One operand of a tile: R rows (or, TR, columns) of the product by BK of the contraction, 2 R BK bytes of LDS a stage.
+//   plain: memory holds R rows of `depth` values; LDS rows of 2 BK bytes, whose sixteen-byte chunks are exchanged so that sixteen lanes
+//          that read one chunk of sixteen rows meet all 64 banks
 //   TR:    memory holds `depth` rows of R values; LDS rows of 2 R bytes, 64-byte pieces exchanged by row & 3: the transposing read
 //          of a half wavefront takes such a piece of four rows
-template <class T, int R, int WAVES, bool TR>
+template <class T, int R, int BK, int WAVES, bool TR>
 struct Operand {
-    static constexpr int kBytes = R * 128, kLoads = kBytes / 1024 / WAVES;     // instructions of a wavefront a stage
-    static constexpr int kChunks = TR ? R / 8 : 8, kRowsAtOnce = 64 / kChunks; // LDS rows that an instruction fills
+    static constexpr int kBytes = R * BK * 2, kLoads = kBytes / 1024 / WAVES;  // instructions of a wavefront a stage
+    static constexpr int kChunks = TR ? R / 8 : BK / 8, kRowsAtOnce = 64 / kChunks;  // LDS rows that an instruction fills
     const T* base;             // the tile's first value
     int64_t depth;             // of the contraction
     uint32_t rows;             // plain: rows that exist, counted from base
@@ -281,61 +311,71 @@ struct Operand {
     uint32_t offset[kLoads];
     int chunk;                 // plain: which chunk this lane brings
 
+    // the place of chunk c in LDS row r
+    static __device__ __forceinline__ int exchanged(int c, int r)
+    {
+        return TR ? c ^ ((r & 3) << 2) : BK == 64 ? c ^ ((r >> 1) & 7) : c ^ ((r >> 2) & 3);
+    }
     __device__ __forceinline__ void init(const T* b, int64_t d, int64_t exist, int64_t stride, int wave, int lane)
     {
+        static_assert(kLoads >= 1 && kBytes % (1024 * WAVES) == 0);
+        static_assert(TR || kRowsAtOnce % 16 == 0 || (BK == 64 && kRowsAtOnce == 8));
         base = b;
         depth = d;
         rows = width = (uint32_t)(exist < R ? exist : R);
         ld = (uint32_t)(stride * 2);
         const int c = lane % kChunks, r0 = wave * kLoads * kRowsAtOnce + lane / kChunks;
-        chunk = c ^ (lane / 8);
 #pragma unroll
         for (int q = 0; q < kLoads; ++q) {
-            const int r = r0 + q * kRowsAtOnce;
-            if (TR) {
-                const uint32_t from = (uint32_t)(c ^ ((r & 3) << 2)) * 8;
-                offset[q] = from < width ? (uint32_t)r * ld + from * 2 : kNowhere;
-            } else {
-                offset[q] = (uint32_t)r * ld + (uint32_t)chunk * 16;
-            }
+            const int r = r0 + q * kRowsAtOnce, from = exchanged(c, r) * 8;
+            if (TR) offset[q] = (uint32_t)from < width ? (uint32_t)r * ld + from * 2 : kNowhere;
+            else offset[q] = (uint32_t)r * ld + from * 2;
         }
+        chunk = c;
     }
     // the stage that starts at k0 (< depth) of the contraction
-    __device__ __forceinline__ void fetch(uint32_t lds, int64_t k0, int wave)
+    __device__ __forceinline__ void fetch(uint32_t lds, int64_t k0, int wave, int lane)
     {
         const int64_t left = depth - k0;
         const uint32_t to = lds + (uint32_t)wave * kLoads * 1024;
         if (TR) {
-            const uint32_t have = (uint32_t)(left < 64 ? left : 64);
+            const uint32_t have = (uint32_t)(left < BK ? left : BK);
             const v4i buffer = buffer_of(base + k0 * (int64_t)(ld / 2), (have - 1) * ld + width * 2);
 #pragma unroll
             for (int q = 0; q < kLoads; ++q) buffer_to_lds(to + q * 1024, offset[q], buffer);
         } else {
             const v4i buffer = buffer_of(base + k0, (rows - 1) * ld + (uint32_t)left * 2);
-            const bool past = chunk * 8 >= left;              // (left is a multiple of eight)
+            if (left >= BK) {
 #pragma unroll
-            for (int q = 0; q < kLoads; ++q) buffer_to_lds(to + q * 1024, past ? kNowhere : offset[q], buffer);
+                for (int q = 0; q < kLoads; ++q) buffer_to_lds(to + q * 1024, offset[q], buffer);
+            } else {                                           // (left is a multiple of eight)
+                const int r0 = wave * kLoads * kRowsAtOnce + lane / kChunks;
+#pragma unroll
+                for (int q = 0; q < kLoads; ++q)
+                    buffer_to_lds(to + q * 1024, exchanged(chunk, r0 + q * kRowsAtOnce) * 8 < left ? offset[q] : kNowhere, buffer);
+            }
         }
     }
 };
 
 // 32 rows by 16 of the contraction as the matrix pipe takes them: lane l holds row l % 32, values 8 (l / 32) .. + 7.
-template <class T, int R, bool TR>
+template <class T, int R, int BK, bool TR>
 __device__ __forceinline__ typename Half8<T>::type fragment(const char* stage, int r0, int k, int lane)
 {
+    typedef Operand<T, R, BK, 1, TR> Op;
     union {
         typename Half8<T>::type v;
         s16x4 s[2];
     } f;
     if constexpr (!TR) {
-        const int r = r0 + (lane & 31), c = (k / 8 + (lane >> 5)) ^ (r & 7);
-        f.v = *reinterpret_cast<const typename Half8<T>::type*>(stage + r * 128 + c * 16);
+        const int r = r0 + (lane & 31), c = Op::exchanged(k / 8 + (lane >> 5), r);
+        f.v = *reinterpret_cast<const typename Half8<T>::type*>(stage + r * (2 * BK) + c * 16);
     } else {
         // Sixteen lanes exchange a block of four rows and sixteen columns: lane 4 j + q brings columns 4 q .. + 3 of row j, lane i gets
         // column i of all four.
         typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
         const int row = k + 8 * (lane >> 5) + ((lane & 15) >> 2), col = r0 + (lane & 16) + 4 * (lane & 3);
-        const char* p = stage + row * (2 * R) + (((col >> 3) ^ ((row & 3) << 2)) << 4) + (col & 7) * 2;
+        const char* p = stage + row * (2 * R) + Op::exchanged(col >> 3, row) * 16 + (col & 7) * 2;
         f.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(s16x4*)p);
         f.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(s16x4*)(p + 4 * (2 * R)));
     }
@@ -349,13 +389,13 @@ __device__ __forceinline__ void stage_ready()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-template <class T, Form F, int BM, int BN, int WM, int WN, int STAGES>
+template <class T, Form F, int BM, int BN, int BK, int WM, int WN>
 __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64) product_tile_kernel(ProductArgs<T> a, int xtiles)
 {
     constexpr int WAVES = (BM / WM) * (BN / WN), THREADS = WAVES * 64;
     constexpr bool TP = F == kOuterSums, TQ = F != kRowsTimesA;
-    typedef Operand<T, BM, WAVES, TP> OpP;
-    typedef Operand<T, BN, WAVES, TQ> OpQ;
+    typedef Operand<T, BM, BK, WAVES, TP> OpP;
+    typedef Operand<T, BN, BK, WAVES, TQ> OpQ;
     constexpr int kStage = OpP::kBytes + OpQ::kBytes, kLoads = OpP::kLoads + OpQ::kLoads;
     extern __shared__ __align__(1024) char tile_lds[];
     typedef typename Half8<T>::type half8;
@@ -387,76 +427,112 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64) product_tile_kerne
         Q.init(F == kRowsTimesA ? A + (int64_t)n0 * a.din : A + n0, depth, Nn - n0, a.din, wave, lane);
     }
     f32x16 acc[WM / 32][WN / 32] = {};
-    const int steps = (int)((depth + 63) / 64);
+    const int steps = (int)((depth + BK - 1) / BK);
     const uint32_t lds = lds_address(tile_lds);
-#pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s) {
-        if (s < steps) {
-            P.fetch(lds + s * kStage, (int64_t)s * 64, wave);
-            Q.fetch(lds + s * kStage + OpP::kBytes, (int64_t)s * 64, wave);
-        }
-    }
-    int slot = 0, ahead = STAGES - 1;
-    for (int i = 0; i < steps; ++i) {
-        if (i + STAGES - 1 <= steps) stage_ready<(STAGES - 2) * kLoads>();
-        else stage_ready<0>();
-        if (i + STAGES - 1 < steps) {
-            const int64_t k0 = (int64_t)(i + STAGES - 1) * 64;
-            P.fetch(lds + ahead * kStage, k0, wave);
-            Q.fetch(lds + ahead * kStage + OpP::kBytes, k0, wave);
-        }
-        const char* stage = tile_lds + slot * kStage;
-#pragma unroll
-        for (int k = 0; k < 64; k += 16) {
-            half8 p[WM / 32], q[WN / 32];
-#pragma unroll
-            for (int u = 0; u < WM / 32; ++u) p[u] = fragment<T, BM, TP>(stage, wm + 32 * u, k, lane);
-#pragma unroll
-            for (int u = 0; u < WN / 32; ++u) q[u] = fragment<T, BN, TQ>(stage + OpP::kBytes, wn + 32 * u, k, lane);
-#pragma unroll
-            for (int u = 0; u < WM / 32; ++u)
-#pragma unroll
-                for (int v = 0; v < WN / 32; ++v) acc[u][v] = mfma(q[v], p[u], acc[u][v]);
-        }
-        slot = slot + 1 == STAGES ? 0 : slot + 1;
-        ahead = ahead + 1 == STAGES ? 0 : ahead + 1;
-    }
-    // a lane holds row wm + 32 u + lane % 32 of the tile, four consecutive columns at a time
-    union Four {
-        uint2 w;
-        T e[4];
+    auto fetch = [&](int i) {                       // stage i of the contraction
+        const int64_t k0 = (int64_t)i * BK;
+        P.fetch(lds + (i & 1) * kStage, k0, wave, lane);
+        Q.fetch(lds + (i & 1) * kStage + OpP::kBytes, k0, wave, lane);
     };
+    half8 p[2][WM / 32], q[2][WN / 32];
+    auto read = [&](int i, int k, int to) {
+        const char* stage = tile_lds + (i & 1) * kStage;
 #pragma unroll
-    for (int u = 0; u < WM / 32; ++u) {
-        const int m = wm + 32 * u + (lane & 31);
-        const int64_t row = F == kOuterSums ? m0 + m : first + m;
-        if (row >= (F == kOuterSums ? a.dout : end)) continue;
-        T* out = F == kOuterSums ? a.out + ((int64_t)e * a.dout + row) * a.din : a.out + row * a.ldo;
+        for (int u = 0; u < WM / 32; ++u) p[to][u] = fragment<T, BM, BK, TP>(stage, wm + 32 * u, k, lane);
 #pragma unroll
-        for (int v = 0; v < WN / 32; ++v) {
+        for (int u = 0; u < WN / 32; ++u) q[to][u] = fragment<T, BN, BK, TQ>(stage + OpP::kBytes, wn + 32 * u, k, lane);
+    };
+    auto multiply = [&](int from) {
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int n = n0 + wn + 32 * v + 8 * g + 4 * (lane >> 5);
-                if (n >= Nn) continue;
-                Four y, z, r, c;
-                if (F == kRowsTimesA) {
-                    if (a.bias) c.w = *reinterpret_cast<const uint2*>(a.bias + (int64_t)e * a.dout + n);
-                    if (a.residual) r.w = *reinterpret_cast<const uint2*>(a.residual + row * a.ldr + n);
-                }
+        for (int u = 0; u < WM / 32; ++u)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float x = acc[u][v][4 * g + j];
-                    if (F == kRowsTimesA) {
-                        if (a.bias) x += (float)c.e[j];
-                        z.e[j] = (T)x;
-                        x = activate(x, a.act);
-                        if (a.residual) x += (float)r.e[j];
-                    }
-                    y.e[j] = (T)x;
-                }
-                if (F == kRowsTimesA && a.pre) *reinterpret_cast<uint2*>(a.pre + row * a.ldpre + n) = z.w;
-                *reinterpret_cast<uint2*>(out + n) = y.w;
+            for (int v = 0; v < WN / 32; ++v) acc[u][v] = mfma(q[from][v], p[from][u], acc[u][v]);
+    };
+    if (steps > 0) {
+        fetch(0);
+        stage_ready<0>();
+        if (steps > 1) fetch(1);
+        read(0, 0, 0);
+        for (int i = 0; i < steps; ++i) {
+#pragma unroll
+            for (int j = 0; j < BK / 16 - 1; ++j) {
+                read(i, 16 * (j + 1), (j + 1) & 1);
+                multiply(j & 1);
             }
+            // The last fragments of this stage are in registers: its buffer is free, and the next stage's first fragments and
+            // everyone's arrival hide behind their products.
+            if (i + 1 < steps) {
+                stage_ready<0>();
+                if (i + 2 < steps) fetch(i + 2);
+                read(i + 1, 0, 0);
+            }
+            multiply(1);
+        }
+    }
+    // Results go out by rows: a wavefront's 32 x WN values change from the pipe's layout (lane: row, four columns at a time) to eight
+    // columns a lane through LDS rows of WN + 4 floats, which keep sixteen lanes on sixteen places both ways.
+    constexpr int kRow = WN + 4, kLanes = WN / 8, kAtOnce = 64 / kLanes;
+    static_assert(WAVES * 32 * kRow * 4 <= 2 * kStage);
+    stage_ready<0>();                               // no one reads the stages any more
+    float* turned = reinterpret_cast<float*>(tile_lds) + wave * 32 * kRow;
+    const int n = n0 + wn + lane % kLanes * 8;
+    Piece<T> c;
+    if (F == kRowsTimesA && a.bias && n < Nn) c.load(a.bias + (int64_t)e * a.dout + n);
+    const int64_t rows_end = F == kOuterSums ? a.dout : end;
+#pragma unroll 1
+    for (int u = 0; u < WM / 32; ++u) {
+        const int64_t row0 = (F == kOuterSums ? m0 : first) + wm + 32 * u;
+        if (row0 >= rows_end) break;
+#pragma unroll
+        for (int w = 0; w < WM / 32; ++w) {
+            if (w != u) continue;
+#pragma unroll
+            for (int v = 0; v < WN / 32; ++v)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const float4 x = make_float4(acc[w][v][4 * g], acc[w][v][4 * g + 1], acc[w][v][4 * g + 2], acc[w][v][4 * g + 3]);
+                    *reinterpret_cast<float4*>(turned + (lane & 31) * kRow + 32 * v + 8 * g + 4 * (lane >> 5)) = x;
+                }
+        }
+#pragma unroll 1
+        for (int r = lane / kLanes; r < 32; r += kAtOnce) {
+            const int64_t row = row0 + r;
+            if (row >= rows_end || n >= Nn) continue;
+            float x[8];
+            *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(turned + r * kRow + lane % kLanes * 8);
+            *reinterpret_cast<float4*>(x + 4) = *reinterpret_cast<const float4*>(turned + r * kRow + lane % kLanes * 8 + 4);
+            Piece<T> y, z, d;
+            if (F == kRowsTimesA) {
+                if (a.residual) d.load(a.residual + row * a.ldr + n);
+                if (a.bias)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[j] += (float)c.e[j];
+                if (a.pre) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) z.e[j] = (T)x[j];
+                    z.store(a.pre + row * a.ldpre + n);
+                }
+                if (a.act == SOM_ACT_SILU) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[j] = activate<T>(x[j], SOM_ACT_SILU);
+                } else if (a.act == SOM_ACT_GELU) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[j] = activate<T>(x[j], SOM_ACT_GELU);
+                } else if (a.act == SOM_ACT_GELU_TANH) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[j] = activate<T>(x[j], SOM_ACT_GELU_TANH);
+                } else if (a.act == SOM_ACT_RELU) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[j] = activate<T>(x[j], SOM_ACT_RELU);
+                }
+                if (a.residual)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[j] += (float)d.e[j];
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y.e[j] = (T)x[j];
+            T* out = F == kOuterSums ? a.out + ((int64_t)e * a.dout + row) * a.din : a.out + row * a.ldo;
+            y.store(out + n);
         }
     }
 }
@@ -469,7 +545,7 @@ __global__ void __launch_bounds__(256) slope_kernel(const T* __restrict__ dY, in
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * dout; i += (int64_t)gridDim.x * 256) {
         const int64_t s = i / dout;
         const int n = (int)(i - s * dout);
-        dz[i] = (T)((float)dY[s * lddy + n] * slope((float)pre[s * ldpre + n], act));
+        dz[i] = (T)((float)dY[s * lddy + n] * Math<sizeof(T) == 4>::slope((float)pre[s * ldpre + n], act));
     }
 }
 
@@ -507,13 +583,13 @@ static bool product_aligned(const ProductArgs<T>& a)
            a.ldpre % 8 == 0 && sixteen(a.P) && sixteen(a.Q) && sixteen(a.out) && sixteen(a.bias) && sixteen(a.residual) && sixteen(a.pre);
 }
 
-template <class T, Form F, int BM, int BN, int WM, int WN, int STAGES>
+template <class T, Form F, int BM, int BN, int BK, int WM, int WN>
 static int product_tile_launch(som_ctx* ctx, const ProductArgs<T>& a, const char* what)
 {
-    constexpr int lds = STAGES * (BM + BN) * 128;
+    constexpr int lds = 2 * (BM + BN) * BK * 2;
     static bool attr_set_dev[kMaxDevices] = {};
     bool& attr_set = attr_set_dev[ctx->device];
-    auto kern = product_tile_kernel<T, F, BM, BN, WM, WN, STAGES>;
+    auto kern = product_tile_kernel<T, F, BM, BN, BK, WM, WN>;
     if (!attr_set) {
         if (int rc = check_hip(ctx, hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds),
                                "raising the dynamic LDS limit"))
@@ -530,7 +606,9 @@ template <class T, Form F>
 static int product_launch(som_ctx* ctx, const ProductArgs<T>& a, const char* what)
 {
     if constexpr (sizeof(T) == 2) {
-        if (product_aligned(a)) return product_tile_launch<T, F, 256, 256, 128, 64, 2>(ctx, a, what);
+        if (product_aligned(a)) {
+            return product_tile_launch<T, F, 256, 256, 64, 128, 64>(ctx, a, what);
+        }
     }
     const unsigned nx = (unsigned)(((F == kRowsTimesA ? a.dout : a.din) + 63) / 64);
     dim3 grid;
