@@ -8,6 +8,8 @@
 // sums are taken by the matrix pipe in float32; float32 rows go through its float32 form.
 #include "som_rows.hpp"
 
+#include <type_traits>
+
 namespace som {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -28,7 +30,7 @@ struct ProductArgs {
     const T* Q;                // A, A, X
     int64_t ldq;               // X only
     const int32_t* offsets;    // null: one node
-    int64_t rows;
+    int rows;
     int32_t K, din, dout;
     const T* bias;
     const T* residual;
@@ -106,7 +108,7 @@ __device__ __forceinline__ float activate(float z, int act)
 }
 
 // Rows [lo, hi) of group e, inside [0, rows) whatever the offsets hold.
-__device__ __forceinline__ void group_rows(const int32_t* __restrict__ offsets, int e, int64_t rows, int64_t& lo, int64_t& hi)
+__device__ __forceinline__ void group_rows(const int32_t* __restrict__ offsets, int e, int rows, int& lo, int& hi)
 {
     if (!offsets) {
         lo = 0;
@@ -119,53 +121,66 @@ __device__ __forceinline__ void group_rows(const int32_t* __restrict__ offsets, 
     hi = hi < lo ? lo : hi > rows ? rows : hi;
 }
 
-// Tile `tile` of all groups' tiles of BM rows, in the groups' order: its group and its first row.  Called by a whole
-// workgroup; false when there are fewer tiles.
-template <int BM, int THREADS>
-__device__ __forceinline__ bool find_tile(const int32_t* __restrict__ offsets, int K, int64_t rows, int64_t tile, int& e, int64_t& first, int64_t& end)
+// Sum over a workgroup.
+template <int THREADS>
+__device__ __forceinline__ uint2 sum_all(uint2 v)
 {
-    __shared__ int sums[THREADS / 64];
-    __shared__ int found[2];
-    if (!offsets) {
-        e = 0;
-        first = tile * BM;
-        end = rows;
-        return first < rows;
+    __shared__ uint2 sums[THREADS / 64];
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        v.x += __shfl_xor(v.x, o);
+        v.y += __shfl_xor(v.y, o);
     }
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = v;
+    __syncthreads();
+    uint2 all = make_uint2(0u, 0u);
+    for (int w = 0; w < THREADS / 64; ++w) {
+        all.x += sums[w].x;
+        all.y += sums[w].y;
+    }
+    return all;
+}
+
+// The group that has the item number `item` when the groups' items are counted in order (items_of(rows): how many a group of so many
+// rows has), and which of its items that is.  Called by a whole workgroup; -1 when there are fewer.
+template <int THREADS, class Items>
+__device__ __forceinline__ int find_group(const int32_t* __restrict__ offsets, int K, int rows, Items items_of, unsigned item, int& which)
+{
+    __shared__ unsigned sums[THREADS / 64];
+    __shared__ int found[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     if (tid == 0) found[0] = -1;
-    int64_t before = 0;
+    unsigned before = 0;
     for (int e0 = 0; e0 < K; e0 += THREADS) {
-        int64_t lo = 0, hi = 0;
-        if (e0 + tid < K) group_rows(offsets, e0 + tid, rows, lo, hi);
-        const int mine = (int)((hi - lo + BM - 1) / BM);
-        int incl = mine;
+        unsigned mine = 0;
+        if (e0 + tid < K) {
+            int lo, hi;
+            group_rows(offsets, e0 + tid, rows, lo, hi);
+            mine = items_of((unsigned)(hi - lo));
+        }
+        unsigned incl = mine;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
-            const int x = __shfl_up(incl, o);
-            if (lane >= o) incl += x;
+            const unsigned v = __shfl_up(incl, o);
+            if (lane >= o) incl += v;
         }
         __syncthreads();                          // sums and found of the round before have been read
         if (lane == 63) sums[wave] = incl;
         __syncthreads();
-        int64_t at = before + incl - mine;
+        unsigned at = before + incl - mine;
         for (int w = 0; w < THREADS / 64; ++w) {
             if (w < wave) at += sums[w];
             before += sums[w];
         }
-        if (tile >= at && tile < at + mine) {
+        if (item >= at && item < at + mine) {
             found[0] = e0 + tid;
-            found[1] = (int)(tile - at);
+            found[1] = (int)(item - at);
         }
-        if (before > tile) break;
+        if (before > item) break;
     }
     __syncthreads();
-    if (found[0] < 0) return false;
-    e = found[0];
-    int64_t lo;
-    group_rows(offsets, e, rows, lo, end);
-    first = lo + (int64_t)found[1] * BM;
-    return true;
+    which = found[1];
+    return found[0];
 }
 
 __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
@@ -189,32 +204,33 @@ __global__ void __launch_bounds__(256) product_any_kernel(ProductArgs<T> a)
     constexpr int BM = 64, BN = 64, BK = 32, PAD = sizeof(T) == 2 ? 8 : 1;
     __shared__ __align__(16) T P[BM][BK + PAD], Q[BN][BK + PAD];
     const int M = F == kOuterSums ? a.dout : 0, Nn = F == kRowsTimesA ? a.dout : a.din;
-    int e;
-    int64_t first, end;
-    int64_t m0;
+    int e, first, end, m0 = 0;
     if (F == kOuterSums) {
         e = blockIdx.z;
-        m0 = (int64_t)blockIdx.y * BM;
+        m0 = blockIdx.y * BM;
         group_rows(a.offsets, e, a.rows, first, end);
     } else {
-        if (!find_tile<BM, 256>(a.offsets, a.K, a.rows, (int64_t)blockIdx.y + (int64_t)blockIdx.z * gridDim.y, e, first, end)) return;
-        m0 = 0;
+        int which;
+        e = find_group<256>(a.offsets, a.K, a.rows, [](unsigned n) { return (n + BM - 1) / BM; }, blockIdx.y + blockIdx.z * gridDim.y, which);
+        if (e < 0) return;
+        group_rows(a.offsets, e, a.rows, first, end);
+        first += which * BM;
     }
     const int n0 = blockIdx.x * BN;
     const T* A = F == kOuterSums ? nullptr : a.Q + (int64_t)e * a.dout * a.din;
-    const int64_t depth = F == kRowsTimesA ? a.din : F == kRowsTimesAt ? a.dout : end - first;
+    const int depth = F == kRowsTimesA ? a.din : F == kRowsTimesAt ? a.dout : end - first;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int wm = (wave & 1) * 32, wn = (wave >> 1) * 32;
     f32x16 acc = {};
-    for (int64_t k0 = 0; k0 < depth; k0 += BK) {
+    for (int k0 = 0; k0 < depth; k0 += BK) {
         __syncthreads();
         for (int i = threadIdx.x; i < BM * BK; i += 256) {
             if (F == kOuterSums) {                                   // consecutive lanes take consecutive m
                 const int m = i % BM, k = i / BM;
-                P[m][k] = m0 + m < M && k0 + k < depth ? a.P[(first + k0 + k) * a.ldp + m0 + m] : (T)0.0f;
+                P[m][k] = m0 + m < M && k0 + k < depth ? a.P[(int64_t)(first + k0 + k) * a.ldp + m0 + m] : (T)0.0f;
             } else {
                 const int k = i % BK, m = i / BK;
-                P[m][k] = first + m < end && k0 + k < depth ? a.P[(first + m) * a.ldp + k0 + k] : (T)0.0f;
+                P[m][k] = first + m < end && k0 + k < depth ? a.P[(int64_t)(first + m) * a.ldp + k0 + k] : (T)0.0f;
             }
         }
         for (int i = threadIdx.x; i < BN * BK; i += 256) {
@@ -223,7 +239,7 @@ __global__ void __launch_bounds__(256) product_any_kernel(ProductArgs<T> a)
                 Q[n][k] = n0 + n < Nn && k0 + k < depth ? A[(int64_t)(n0 + n) * a.din + k0 + k] : (T)0.0f;
             } else {
                 const int n = i % BN, k = i / BN;
-                const T* row = F == kRowsTimesAt ? A + (k0 + k) * a.din : a.Q + (first + k0 + k) * a.ldq;
+                const T* row = F == kRowsTimesAt ? A + (int64_t)(k0 + k) * a.din : a.Q + (int64_t)(first + k0 + k) * a.ldq;
                 Q[n][k] = n0 + n < Nn && k0 + k < depth ? row[n0 + n] : (T)0.0f;
             }
         }
@@ -253,7 +269,7 @@ __global__ void __launch_bounds__(256) product_any_kernel(ProductArgs<T> a)
             if (m0 + m < M) a.out[((int64_t)e * a.dout + m0 + m) * a.din + n] = (T)z;
             continue;
         }
-        const int64_t s = first + m;
+        const int64_t s = (int64_t)first + m;
         if (s >= end) continue;
         if (F == kRowsTimesA) {
             z += c;
@@ -304,7 +320,7 @@ struct Operand {
     static constexpr int kBytes = R * BK * 2, kLoads = kBytes / 1024 / WAVES;  // instructions of a wavefront a stage
     static constexpr int kChunks = TR ? R / 8 : BK / 8, kRowsAtOnce = 64 / kChunks;  // LDS rows that an instruction fills
     const T* base;             // the tile's first value
-    int64_t depth;             // of the contraction
+    int depth;                 // of the contraction
     uint32_t rows;             // plain: rows that exist, counted from base
     uint32_t width;            // TR: values that exist in a row, counted from base
     uint32_t ld;               // bytes
@@ -316,7 +332,7 @@ struct Operand {
     {
         return TR ? c ^ ((r & 3) << 2) : BK == 64 ? c ^ ((r >> 1) & 7) : c ^ ((r >> 2) & 3);
     }
-    __device__ __forceinline__ void init(const T* b, int64_t d, int64_t exist, int64_t stride, int wave, int lane)
+    __device__ __forceinline__ void init(const T* b, int d, int exist, int64_t stride, int wave, int lane)
     {
         static_assert(kLoads >= 1 && kBytes % (1024 * WAVES) == 0);
         static_assert(TR || kRowsAtOnce % 16 == 0 || (BK == 64 && kRowsAtOnce == 8));
@@ -334,13 +350,13 @@ struct Operand {
         chunk = c;
     }
     // the stage that starts at k0 (< depth) of the contraction
-    __device__ __forceinline__ void fetch(uint32_t lds, int64_t k0, int wave, int lane)
+    __device__ __forceinline__ void fetch(uint32_t lds, int k0, int wave, int lane)
     {
-        const int64_t left = depth - k0;
+        const int left = depth - k0;
         const uint32_t to = lds + (uint32_t)wave * kLoads * 1024;
         if (TR) {
             const uint32_t have = (uint32_t)(left < BK ? left : BK);
-            const v4i buffer = buffer_of(base + k0 * (int64_t)(ld / 2), (have - 1) * ld + width * 2);
+            const v4i buffer = buffer_of((const char*)base + (uint64_t)(uint32_t)k0 * ld, (have - 1) * ld + width * 2);
 #pragma unroll
             for (int q = 0; q < kLoads; ++q) buffer_to_lds(to + q * 1024, offset[q], buffer);
         } else {
@@ -389,8 +405,18 @@ __device__ __forceinline__ void stage_ready()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
+// Tile number `tile` of `rows` rows of `wide` tiles, taken in bands of up to eight columns: a die's 32 workgroups work on some four rows and
+// eight columns at a time, whose operands its cache holds (8192 x 8192 x 8192 in rows of 32 tiles 970 us, in bands 908).
+__device__ __forceinline__ unsigned banded(unsigned tile, unsigned rows, unsigned wide, unsigned& x)
+{
+    const unsigned bands = (wide + 7) / 8, w = (wide + bands - 1) / bands, band = tile / (rows * w), rest = tile - band * rows * w;
+    const unsigned mine = wide - band * w < w ? wide - band * w : w;
+    x = band * w + rest % mine;
+    return rest / mine;
+}
+
 template <class T, Form F, int BM, int BN, int BK, int WM, int WN>
-__global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64) product_tile_kernel(ProductArgs<T> a, int xtiles)
+__global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64) product_tile_kernel(ProductArgs<T> a, unsigned xtiles)
 {
     constexpr int WAVES = (BM / WM) * (BN / WN), THREADS = WAVES * 64;
     constexpr bool TP = F == kOuterSums, TQ = F != kRowsTimesA;
@@ -403,71 +429,110 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64) product_tile_kerne
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN) * WN;
     const int Nn = F == kRowsTimesA ? a.dout : a.din;
-    int e;
-    int64_t first, end, m0 = 0;
-    const int nt = blockIdx.x % xtiles, mt = blockIdx.x / xtiles;
-    const int n0 = nt * BN;
+    int e, first, end, m0 = 0;
+    unsigned x;
+    // The chip's eight dies take workgroups in turn; each gets a run of tiles that share operands in its cache.
+    const unsigned xcd = blockIdx.x % 8, turn = blockIdx.x / 8;
     if (F == kOuterSums) {
-        const int ytiles = (a.dout + BM - 1) / BM;
-        e = mt / ytiles;
-        m0 = (int64_t)(mt % ytiles) * BM;
+        const unsigned ytiles = (a.dout + BM - 1) / BM, each = ytiles * xtiles, total = a.K * each, run = (total + 7) / 8;
+        const unsigned tile = xcd * run + turn;
+        if (turn >= run || tile >= total) return;
+        e = tile / each;
+        m0 = banded(tile % each, ytiles, xtiles, x) * BM;
         group_rows(a.offsets, e, a.rows, first, end);
     } else {
-        if (!find_tile<BM, THREADS>(a.offsets, a.K, a.rows, mt, e, first, end)) return;
+        // whole tiles first, the groups' last ones, which take less time, when those run out
+        uint2 rows_of_tiles = make_uint2(0u, 0u);
+        for (int k = threadIdx.x; k < a.K; k += THREADS) {
+            group_rows(a.offsets, k, a.rows, first, end);
+            rows_of_tiles.x += (unsigned)(end - first) / BM;
+            rows_of_tiles.y += (unsigned)(end - first) % BM ? 1u : 0u;
+        }
+        rows_of_tiles = sum_all<THREADS>(rows_of_tiles);
+        const unsigned whole = rows_of_tiles.x * xtiles, run = (whole + 7) / 8, at = xcd * run;
+        const unsigned mine = at < whole ? (whole - at < run ? whole - at : run) : 0u;
+        int which;
+        if (turn < mine) {
+            const unsigned row = banded(at + turn, rows_of_tiles.x, xtiles, x);
+            e = find_group<THREADS>(a.offsets, a.K, a.rows, [](unsigned n) { return n / BM; }, row, which);
+            group_rows(a.offsets, e, a.rows, first, end);
+            first += which * BM;
+        } else {
+            const unsigned rest = rows_of_tiles.y * xtiles, last = (rest + 7) / 8, tile = (7 - xcd) * last + turn - mine;
+            if (turn - mine >= last || tile >= rest) return;
+            const unsigned row = banded(tile, rows_of_tiles.y, xtiles, x);
+            e = find_group<THREADS>(a.offsets, a.K, a.rows, [](unsigned n) { return n % BM ? 1u : 0u; }, row, which);
+            group_rows(a.offsets, e, a.rows, first, end);
+            first = end - (end - first) % BM;
+        }
     }
+    e = __builtin_amdgcn_readfirstlane(e);
+    first = __builtin_amdgcn_readfirstlane(first);
+    end = __builtin_amdgcn_readfirstlane(end);
+    const int n0 = __builtin_amdgcn_readfirstlane(x) * BN;
     OpP P;
     OpQ Q;
-    const int64_t depth = F == kRowsTimesA ? a.din : F == kRowsTimesAt ? a.dout : end - first;
+    const int depth = F == kRowsTimesA ? a.din : F == kRowsTimesAt ? a.dout : end - first;
     if (F == kOuterSums) {
-        P.init(a.P + first * a.ldp + m0, depth, a.dout - m0, a.ldp, wave, lane);
-        Q.init(a.Q + first * a.ldq + n0, depth, a.din - n0, a.ldq, wave, lane);
+        P.init(a.P + (int64_t)first * a.ldp + m0, depth, a.dout - m0, a.ldp, wave, lane);
+        Q.init(a.Q + (int64_t)first * a.ldq + n0, depth, a.din - n0, a.ldq, wave, lane);
     } else {
-        P.init(a.P + first * a.ldp, depth, end - first, a.ldp, wave, lane);
+        P.init(a.P + (int64_t)first * a.ldp, depth, end - first, a.ldp, wave, lane);
         const T* A = a.Q + (int64_t)e * a.dout * a.din;
         Q.init(F == kRowsTimesA ? A + (int64_t)n0 * a.din : A + n0, depth, Nn - n0, a.din, wave, lane);
     }
     f32x16 acc[WM / 32][WN / 32] = {};
-    const int steps = (int)((depth + BK - 1) / BK);
+    const int steps = (depth + BK - 1) / BK;
     const uint32_t lds = lds_address(tile_lds);
+    // blocks of 32 rows that this wavefront has; the columns' ends are left to zeros and to the stores
+    const int have = ((F == kOuterSums ? a.dout - m0 : end - first) - wm + 31) / 32;
     auto fetch = [&](int i) {                       // stage i of the contraction
-        const int64_t k0 = (int64_t)i * BK;
-        P.fetch(lds + (i & 1) * kStage, k0, wave, lane);
-        Q.fetch(lds + (i & 1) * kStage + OpP::kBytes, k0, wave, lane);
+        P.fetch(lds + (i & 1) * kStage, i * BK, wave, lane);
+        Q.fetch(lds + (i & 1) * kStage + OpP::kBytes, i * BK, wave, lane);
     };
     half8 p[2][WM / 32], q[2][WN / 32];
-    auto read = [&](int i, int k, int to) {
+    auto read = [&](auto whole, int i, int k, int to) {
         const char* stage = tile_lds + (i & 1) * kStage;
 #pragma unroll
-        for (int u = 0; u < WM / 32; ++u) p[to][u] = fragment<T, BM, BK, TP>(stage, wm + 32 * u, k, lane);
-#pragma unroll
-        for (int u = 0; u < WN / 32; ++u) q[to][u] = fragment<T, BN, BK, TQ>(stage + OpP::kBytes, wn + 32 * u, k, lane);
-    };
-    auto multiply = [&](int from) {
+        for (int v = 0; v < WN / 32; ++v) q[to][v] = fragment<T, BN, BK, TQ>(stage + OpP::kBytes, wn + 32 * v, k, lane);
 #pragma unroll
         for (int u = 0; u < WM / 32; ++u)
-#pragma unroll
-            for (int v = 0; v < WN / 32; ++v) acc[u][v] = mfma(q[from][v], p[from][u], acc[u][v]);
+            if (whole || u < have) p[to][u] = fragment<T, BM, BK, TP>(stage, wm + 32 * u, k, lane);
+        __builtin_amdgcn_sched_barrier(0);          // (the scheduler would put the reads back to where their values are needed)
     };
-    if (steps > 0) {
-        fetch(0);
-        stage_ready<0>();
-        if (steps > 1) fetch(1);
-        read(0, 0, 0);
+    auto multiply = [&](auto whole, int from) {
+#pragma unroll
+        for (int u = 0; u < WM / 32; ++u)
+            if (whole || u < have)
+#pragma unroll
+                for (int v = 0; v < WN / 32; ++v) acc[u][v] = mfma(q[from][v], p[from][u], acc[u][v]);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto contract = [&](auto whole) {
+        read(whole, 0, 0, 0);
         for (int i = 0; i < steps; ++i) {
 #pragma unroll
             for (int j = 0; j < BK / 16 - 1; ++j) {
-                read(i, 16 * (j + 1), (j + 1) & 1);
-                multiply(j & 1);
+                read(whole, i, 16 * (j + 1), (j + 1) & 1);
+                multiply(whole, j & 1);
             }
             // The last fragments of this stage are in registers: its buffer is free, and the next stage's first fragments and
             // everyone's arrival hide behind their products.
             if (i + 1 < steps) {
                 stage_ready<0>();
                 if (i + 2 < steps) fetch(i + 2);
-                read(i + 1, 0, 0);
+                read(whole, i + 1, 0, 0);
             }
-            multiply(1);
+            multiply(whole, 1);
         }
+    };
+    if (steps > 0) {
+        fetch(0);
+        stage_ready<0>();
+        if (steps > 1) fetch(1);
+        // a group's last tile leaves out the blocks of rows that it does not have
+        if (have >= WM / 32) contract(std::true_type{});
+        else contract(std::false_type{});
     }
     // Results go out by rows: a wavefront's 32 x WN values change from the pipe's layout (lane: row, four columns at a time) to eight
     // columns a lane through LDS rows of WN + 4 floats, which keep sixteen lanes on sixteen places both ways.
@@ -478,11 +543,11 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64) product_tile_kerne
     const int n = n0 + wn + lane % kLanes * 8;
     Piece<T> c;
     if (F == kRowsTimesA && a.bias && n < Nn) c.load(a.bias + (int64_t)e * a.dout + n);
-    const int64_t rows_end = F == kOuterSums ? a.dout : end;
+    const int rows_end = F == kOuterSums ? a.dout : end;
 #pragma unroll 1
     for (int u = 0; u < WM / 32; ++u) {
-        const int64_t row0 = (F == kOuterSums ? m0 : first) + wm + 32 * u;
-        if (row0 >= rows_end) break;
+        if (u >= have) break;
+        const int64_t row0 = (int64_t)(F == kOuterSums ? m0 : first) + wm + 32 * u;
 #pragma unroll
         for (int w = 0; w < WM / 32; ++w) {
             if (w != u) continue;
@@ -556,8 +621,8 @@ __global__ void __launch_bounds__(256) bias_grad_kernel(const T* __restrict__ dz
 {
     __shared__ float run[4][64];
     const int e = blockIdx.y, l = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockIdx.x * 64 + l;
-    int64_t lo, hi;
-    group_rows(offsets, e, rows, lo, hi);
+    int lo, hi;
+    group_rows(offsets, e, (int)rows, lo, hi);
     float s = 0.0f;
     if (n < dout)
         for (int64_t r = lo + wave; r < hi; r += 4) s += (float)dz[r * lddz + n];
@@ -598,7 +663,7 @@ static int product_tile_launch(som_ctx* ctx, const ProductArgs<T>& a, const char
     }
     const int xtiles = ((F == kRowsTimesA ? a.dout : a.din) + BN - 1) / BN;
     const int64_t ytiles = F == kOuterSums ? (int64_t)a.K * ((a.dout + BM - 1) / BM) : most_tiles(a.rows, a.K, a.offsets, BM);
-    hipLaunchKernelGGL(kern, dim3((unsigned)(xtiles * ytiles)), dim3((BM / WM) * (BN / WN) * 64), lds, ctx->stream, a, xtiles);
+    hipLaunchKernelGGL(kern, dim3((unsigned)((xtiles * ytiles + 7) / 8 + 2) * 8), dim3((BM / WM) * (BN / WN) * 64), lds, ctx->stream, a, xtiles);
     return check_hip(ctx, hipGetLastError(), what);
 }
 
@@ -631,7 +696,7 @@ static int product_typed(som_ctx* ctx, const NodeProduct& p)
     a.ldp = p.ldx;
     a.Q = (const T*)p.A;
     a.offsets = p.offsets;
-    a.rows = p.rows;
+    a.rows = (int)p.rows;
     a.K = p.K;
     a.din = p.din;
     a.dout = p.dout;
@@ -664,7 +729,7 @@ static int product_grad_typed(som_ctx* ctx, const NodeProductGrad& p)
     a.P = dz;
     a.ldp = lddz;
     a.offsets = p.offsets;
-    a.rows = p.rows;
+    a.rows = (int)p.rows;
     a.K = p.K;
     a.din = p.din;
     a.dout = p.dout;
