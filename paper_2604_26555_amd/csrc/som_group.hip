@@ -131,14 +131,6 @@ static dim3 row_grid(int64_t items, int each)
     return dim3((unsigned)(groups < most ? groups : most));
 }
 
-// Lanes that share a row of `pieces` pieces: a power of two, at most `most`.
-static int row_lanes(int64_t pieces, int most)
-{
-    int l = 1;
-    while (l < most && l < pieces) l *= 2;
-    return l;
-}
-
 template <class T, int LANES>
 __global__ void __launch_bounds__(256) dispatch_kernel(const T* __restrict__ X, int64_t rows, int D, int64_t ldx, const int32_t* __restrict__ slot, int k,
                                                        const float* __restrict__ weight, T* __restrict__ Y, int64_t places, int64_t ldy)

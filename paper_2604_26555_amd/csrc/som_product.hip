@@ -40,6 +40,10 @@ struct ProductArgs {
     T* out;                    // Y, dX, dA
     int64_t ldo;
     int act;
+    // Sums over rows (kOuterSums): a group's rows are taken in runs of `run`, every run's sum by another workgroup; with more than one run
+    // a group, the sums go to `parts` in float32 (runs_slot) and are added up in order afterwards
+    int run;
+    float* parts;
 };
 
 // Where a factor has reached its limit the product with z is formed from the limit, so that infinities give what the function
@@ -183,6 +187,13 @@ __device__ __forceinline__ int find_group(const int32_t* __restrict__ offsets, i
     return found[0];
 }
 
+// Runs of `run` rows that a group of n rows has, and which part a run's sum goes to when there are more than one: the run starts at
+// `first` of a group that starts at lo.  (No other run has the same: runs behind a group's first one that start within the same `run`
+// rows would be of one group, and so would two first ones of groups with more than `run` rows.)
+__device__ __forceinline__ unsigned runs_of(unsigned n, unsigned run) { return n <= run ? 1u : (n - 1) / run + 1u; }
+__device__ __forceinline__ int64_t run_slot(int first, int lo, int run) { return 2 * (int64_t)(first / run) + (first == lo); }
+static int64_t run_slots(int64_t rows, int run) { return 2 * (rows / run + 1); }
+
 __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x16 mfma(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 
@@ -204,13 +215,21 @@ __global__ void __launch_bounds__(256) product_any_kernel(ProductArgs<T> a)
     constexpr int BM = 64, BN = 64, BK = 32, PAD = sizeof(T) == 2 ? 8 : 1;
     __shared__ __align__(16) T P[BM][BK + PAD], Q[BN][BK + PAD];
     const int M = F == kOuterSums ? a.dout : 0, Nn = F == kRowsTimesA ? a.dout : a.din;
-    int e, first, end, m0 = 0;
+    int e, first, end, m0 = 0, which;
+    float* part = nullptr;
     if (F == kOuterSums) {
-        e = blockIdx.z;
+        const int run = a.run;
+        e = find_group<256>(a.offsets, a.K, a.rows, [run](unsigned n) { return runs_of(n, run); }, blockIdx.z, which);
+        if (e < 0) return;
         m0 = blockIdx.y * BM;
         group_rows(a.offsets, e, a.rows, first, end);
+        if (end - first > run) {
+            const int lo = first;
+            first += which * run;
+            end = end - first > run ? first + run : end;
+            part = a.parts + run_slot(first, lo, run) * ((int64_t)a.dout * a.din);
+        }
     } else {
-        int which;
         e = find_group<256>(a.offsets, a.K, a.rows, [](unsigned n) { return (n + BM - 1) / BM; }, blockIdx.y + blockIdx.z * gridDim.y, which);
         if (e < 0) return;
         group_rows(a.offsets, e, a.rows, first, end);
@@ -266,7 +285,10 @@ __global__ void __launch_bounds__(256) product_any_kernel(ProductArgs<T> a)
         const int m = wm + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5);
         float z = acc[r];
         if (F == kOuterSums) {
-            if (m0 + m < M) a.out[((int64_t)e * a.dout + m0 + m) * a.din + n] = (T)z;
+            if (m0 + m < M) {
+                if (part) part[(int64_t)(m0 + m) * a.din + n] = z;
+                else a.out[((int64_t)e * a.dout + m0 + m) * a.din + n] = (T)z;
+            }
             continue;
         }
         const int64_t s = (int64_t)first + m;
@@ -422,7 +444,7 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64) product_tile_kerne
     constexpr bool TP = F == kOuterSums, TQ = F != kRowsTimesA;
     typedef Operand<T, BM, BK, WAVES, TP> OpP;
     typedef Operand<T, BN, BK, WAVES, TQ> OpQ;
-    constexpr int kStage = OpP::kBytes + OpQ::kBytes, kLoads = OpP::kLoads + OpQ::kLoads;
+    constexpr int kStage = OpP::kBytes + OpQ::kBytes;
     extern __shared__ __align__(1024) char tile_lds[];
     typedef typename Half8<T>::type half8;
 
@@ -433,13 +455,27 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64) product_tile_kerne
     unsigned x;
     // The chip's eight dies take workgroups in turn; each gets a run of tiles that share operands in its cache.
     const unsigned xcd = blockIdx.x % 8, turn = blockIdx.x / 8;
+    float* part = nullptr;
     if (F == kOuterSums) {
-        const unsigned ytiles = (a.dout + BM - 1) / BM, each = ytiles * xtiles, total = a.K * each, run = (total + 7) / 8;
-        const unsigned tile = xcd * run + turn;
-        if (turn >= run || tile >= total) return;
-        e = tile / each;
+        const unsigned run = a.run;
+        uint2 runs = make_uint2(0u, 0u);
+        for (int k = threadIdx.x; k < a.K; k += THREADS) {
+            group_rows(a.offsets, k, a.rows, first, end);
+            runs.x += runs_of(end - first, run);
+        }
+        const unsigned ytiles = (a.dout + BM - 1) / BM, each = ytiles * xtiles, total = sum_all<THREADS>(runs).x * each, share = (total + 7) / 8;
+        const unsigned tile = xcd * share + turn;
+        if (turn >= share || tile >= total) return;
+        int which;
+        e = find_group<THREADS>(a.offsets, a.K, a.rows, [run](unsigned n) { return runs_of(n, run); }, tile / each, which);
         m0 = banded(tile % each, ytiles, xtiles, x) * BM;
         group_rows(a.offsets, e, a.rows, first, end);
+        if (end - first > (int)run) {
+            const int lo = first;
+            first += which * run;
+            end = end - first > (int)run ? first + (int)run : end;
+            part = a.parts + run_slot(first, lo, run) * ((int64_t)a.dout * a.din);
+        }
     } else {
         // whole tiles first, the groups' last ones, which take less time, when those run out
         uint2 rows_of_tiles = make_uint2(0u, 0u);
@@ -594,6 +630,11 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64) product_tile_kerne
 #pragma unroll
                     for (int j = 0; j < 8; ++j) x[j] += (float)d.e[j];
             }
+            if (F == kOuterSums && part) {
+                *reinterpret_cast<float4*>(part + row * a.din + n) = *reinterpret_cast<const float4*>(x);
+                *reinterpret_cast<float4*>(part + row * a.din + n + 4) = *reinterpret_cast<const float4*>(x + 4);
+                continue;
+            }
 #pragma unroll
             for (int j = 0; j < 8; ++j) y.e[j] = (T)x[j];
             T* out = F == kOuterSums ? a.out + ((int64_t)e * a.dout + row) * a.din : a.out + row * a.ldo;
@@ -602,33 +643,73 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64) product_tile_kerne
     }
 }
 
-// dz = dy act'(z), dense
-template <class T>
-__global__ void __launch_bounds__(256) slope_kernel(const T* __restrict__ dY, int64_t lddy, const T* __restrict__ pre, int64_t ldpre, int64_t rows,
-                                                    int32_t dout, int act, T* __restrict__ dz)
+// dz = dy act'(z), dense (where there is an activation: dz not null), and its column sums over a run of a group's rows (dbias not null):
+// LANES lanes of N columns share a row.
+template <class T, int N, int LANES>
+__global__ void __launch_bounds__(256) slope_kernel(const T* __restrict__ dY, int64_t lddy, const T* __restrict__ pre, int64_t ldpre,
+                                                    const int32_t* __restrict__ offsets, int K, int rows, int32_t dout, int act, T* __restrict__ dz,
+                                                    T* __restrict__ dbias, int run, float* __restrict__ parts)
 {
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * dout; i += (int64_t)gridDim.x * 256) {
-        const int64_t s = i / dout;
-        const int n = (int)(i - s * dout);
-        dz[i] = (T)((float)dY[s * lddy + n] * Math<sizeof(T) == 4>::slope((float)pre[s * ldpre + n], act));
+    constexpr int kRows = 256 / LANES;
+    __shared__ float sums[kRows][LANES * N];
+    int which, first, end;
+    const int e = find_group<256>(offsets, K, rows, [run](unsigned n) { return runs_of(n, run); }, blockIdx.y + blockIdx.z * gridDim.y, which);
+    if (e < 0) return;
+    group_rows(offsets, e, rows, first, end);
+    const int lo = first, group = end - first;
+    first += which * run;
+    end = end - first > run ? first + run : end;
+    const int l = threadIdx.x % LANES, c = blockIdx.x * LANES + l;
+    const bool mine = c * N < dout;
+    const int64_t at = mine ? piece_at<T, N>(c, dout) : 0;
+    float s[N] = {};
+    if (mine) {
+        for (int r = first + threadIdx.x / LANES; r < end; r += kRows) {
+            Piece<T, N> g;
+            g.load(dY + (int64_t)r * lddy + at);
+            if (dz) {
+                Piece<T, N> z;
+                z.load(pre + (int64_t)r * ldpre + at);
+#pragma unroll
+                for (int j = 0; j < N; ++j) g.e[j] = (T)((float)g.e[j] * Math<sizeof(T) == 4>::slope((float)z.e[j], act));
+                g.store(dz + (int64_t)r * dout + at);
+            }
+#pragma unroll
+            for (int j = 0; j < N; ++j) s[j] += (float)g.e[j];
+        }
     }
+    if (!dbias) return;
+#pragma unroll
+    for (int j = 0; j < N; ++j) sums[threadIdx.x / LANES][l * N + j] = s[j];
+    __syncthreads();
+    if (threadIdx.x >= LANES || !mine) return;
+    Piece<T, N> out;
+    float* part = group > run ? parts + run_slot(first, lo, run) * dout + at : nullptr;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        float v = 0.0f;
+        for (int r = 0; r < kRows; ++r) v += sums[r][l * N + j];
+        if (part) part[j] = v;
+        out.e[j] = (T)v;
+    }
+    if (!part) out.store(dbias + (int64_t)e * dout + at);
 }
 
-// dc_e: 64 results and 4 runs of rows per workgroup
+// The sums of groups with more than one run, run after run: `count` values a group.
 template <class T>
-__global__ void __launch_bounds__(256) bias_grad_kernel(const T* __restrict__ dz, int64_t lddz, const int32_t* __restrict__ offsets, int64_t rows,
-                                                        int32_t dout, T* __restrict__ dbias)
+__global__ void __launch_bounds__(256) runs_join_kernel(const int32_t* __restrict__ offsets, int K, int rows, int run, const float* __restrict__ parts,
+                                                        int64_t count, T* __restrict__ out)
 {
-    __shared__ float run[4][64];
-    const int e = blockIdx.y, l = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockIdx.x * 64 + l;
-    int lo, hi;
-    group_rows(offsets, e, (int)rows, lo, hi);
-    float s = 0.0f;
-    if (n < dout)
-        for (int64_t r = lo + wave; r < hi; r += 4) s += (float)dz[r * lddz + n];
-    run[wave][l] = s;
-    __syncthreads();
-    if (wave == 0 && n < dout) dbias[(int64_t)e * dout + n] = (T)((run[0][l] + run[1][l]) + (run[2][l] + run[3][l]));
+    int which, lo, hi;
+    const int e = find_group<256>(offsets, K, rows, [run](unsigned n) { return n > (unsigned)run ? 1u : 0u; }, blockIdx.y, which);
+    if (e < 0) return;
+    group_rows(offsets, e, rows, lo, hi);
+    const int runs = (int)runs_of(hi - lo, run);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) {
+        float s = parts[run_slot(lo, lo, run) * count + i];
+        for (int c = 1; c < runs; ++c) s += parts[run_slot(lo + c * run, lo, run) * count + i];
+        out[(int64_t)e * count + i] = (T)s;
+    }
 }
 
 // Tiles of `bm` rows that the groups can have together.
@@ -638,13 +719,29 @@ static int64_t most_tiles(int64_t rows, int32_t K, const int32_t* offsets, int b
     return offsets ? full + (K < rows ? K : rows) : full;
 }
 
+// Runs of `run` rows that the groups can have together.
+static int64_t most_runs(int64_t rows, int32_t K, int run) { return rows / run + K; }
+
+// Rows a run of a sum over rows when a group alone gives `tiles` workgroups: one run a group where the groups fill the chip (longer ones
+// only for a group of eight times its share), shorter ones where they do not.
+static int run_rows(const som_ctx* ctx, int64_t rows, int32_t K, int64_t tiles, int least)
+{
+    const int64_t share = (rows + K - 1) / K, runs = ctx->units / (K * tiles > ctx->units ? ctx->units : K * tiles);
+    int64_t run = runs > 1 ? (share + runs - 1) / runs : K > 1 ? 8 * share : rows;
+    if (runs <= 1 && run < 4096) run = 4096;
+    if (run < least) run = least;
+    if (run * 32000 < rows) run = rows / 32000 + 1;             // (a grid's third dimension)
+    return (int)((run + 63) / 64 * 64 < 0x7fffffc0 ? (run + 63) / 64 * 64 : 0x7fffffc0);
+}
+
 static bool sixteen(const void* p) { return (uintptr_t)p % 16 == 0; }
 
 // What the wide tiles ask of a call: every row of every matrix starts at a multiple of sixteen bytes and has whole chunks of them.
 template <class T>
-static bool product_aligned(const ProductArgs<T>& a)
+static bool product_wide(const ProductArgs<T>& a)
 {
-    return sizeof(T) == 2 && a.din % 8 == 0 && a.dout % 8 == 0 && a.ldp % 8 == 0 && a.ldq % 8 == 0 && a.ldo % 8 == 0 && a.ldr % 8 == 0 &&
+    const bool few = ((a.dout + 255) / 256 * (int64_t)((a.din + 255) / 256 + 1)) * (a.rows / 256 + a.K + 2) < 1 << 22;       // fewer than 2^32 work-items
+    return few && sizeof(T) == 2 && a.din % 8 == 0 && a.dout % 8 == 0 && a.ldp % 8 == 0 && a.ldq % 8 == 0 && a.ldo % 8 == 0 && a.ldr % 8 == 0 &&
            a.ldpre % 8 == 0 && sixteen(a.P) && sixteen(a.Q) && sixteen(a.out) && sixteen(a.bias) && sixteen(a.residual) && sixteen(a.pre);
 }
 
@@ -661,9 +758,9 @@ static int product_tile_launch(som_ctx* ctx, const ProductArgs<T>& a, const char
             return rc;
         attr_set = true;
     }
-    const int xtiles = ((F == kRowsTimesA ? a.dout : a.din) + BN - 1) / BN;
-    const int64_t ytiles = F == kOuterSums ? (int64_t)a.K * ((a.dout + BM - 1) / BM) : most_tiles(a.rows, a.K, a.offsets, BM);
-    hipLaunchKernelGGL(kern, dim3((unsigned)((xtiles * ytiles + 7) / 8 + 2) * 8), dim3((BM / WM) * (BN / WN) * 64), lds, ctx->stream, a, xtiles);
+    const int64_t xtiles = ((F == kRowsTimesA ? a.dout : a.din) + BN - 1) / BN;
+    const int64_t ytiles = F == kOuterSums ? most_runs(a.rows, a.K, a.run) * ((a.dout + BM - 1) / BM) : most_tiles(a.rows, a.K, a.offsets, BM);
+    hipLaunchKernelGGL(kern, dim3((unsigned)((xtiles * ytiles + 7) / 8 + 2) * 8), dim3((BM / WM) * (BN / WN) * 64), lds, ctx->stream, a, (unsigned)xtiles);
     return check_hip(ctx, hipGetLastError(), what);
 }
 
@@ -671,14 +768,12 @@ template <class T, Form F>
 static int product_launch(som_ctx* ctx, const ProductArgs<T>& a, const char* what)
 {
     if constexpr (sizeof(T) == 2) {
-        if (product_aligned(a)) {
-            return product_tile_launch<T, F, 256, 256, 64, 128, 64>(ctx, a, what);
-        }
+        if (product_wide(a)) return product_tile_launch<T, F, 256, 256, 64, 128, 64>(ctx, a, what);
     }
     const unsigned nx = (unsigned)(((F == kRowsTimesA ? a.dout : a.din) + 63) / 64);
     dim3 grid;
     if (F == kOuterSums) {
-        grid = dim3(nx, (unsigned)((a.dout + 63) / 64), (unsigned)a.K);
+        grid = dim3(nx, (unsigned)((a.dout + 63) / 64), (unsigned)most_runs(a.rows, a.K, a.run));
     } else {
         const int64_t tiles = most_tiles(a.rows, a.K, a.offsets, 64);
         const int64_t y = tiles < 32768 ? tiles : 32768;
@@ -711,28 +806,67 @@ static int product_typed(som_ctx* ctx, const NodeProduct& p)
     return product_launch<T, kRowsTimesA>(ctx, a, "product launch");
 }
 
+// Kernel and columns of a workgroup for the slopes and biases of `dout` columns.
+template <class T>
+static auto slope_kernel_for(int32_t dout, int& columns)
+{
+    constexpr int N = Piece<T>::N;
+    const int lanes = dout < N ? row_lanes(dout, 8) : row_lanes((dout + N - 1) / N, 64);
+    columns = lanes * (dout < N ? 1 : N);
+    if (dout < N) return lanes == 1 ? slope_kernel<T, 1, 1> : lanes == 2 ? slope_kernel<T, 1, 2> : lanes == 4 ? slope_kernel<T, 1, 4> : slope_kernel<T, 1, 8>;
+    return lanes == 1   ? slope_kernel<T, N, 1>
+           : lanes == 2 ? slope_kernel<T, N, 2>
+           : lanes == 4 ? slope_kernel<T, N, 4>
+           : lanes == 8 ? slope_kernel<T, N, 8>
+           : lanes == 16 ? slope_kernel<T, N, 16>
+           : lanes == 32 ? slope_kernel<T, N, 32>
+                         : slope_kernel<T, N, 64>;
+}
+
+template <class T>
+static int runs_join(som_ctx* ctx, const int32_t* offsets, int32_t K, int64_t rows, int run, const float* parts, int64_t count, T* out)
+{
+    const int64_t longer = rows / (run + 1), y = longer < K ? longer : K, blocks = (count + 1023) / 1024;        // groups with more than one run, at most
+    if (y == 0) return SOM_OK;
+    hipLaunchKernelGGL(runs_join_kernel<T>, dim3((unsigned)(blocks < 4096 ? blocks : 4096), (unsigned)y), dim3(256), 0, ctx->stream, offsets, K, (int)rows,
+                       run, parts, count, out);
+    return check_hip(ctx, hipGetLastError(), "product gradient join launch");
+}
+
 template <class T>
 static int product_grad_typed(som_ctx* ctx, const NodeProductGrad& p)
 {
-    const T* dz = (const T*)p.dY;
-    int64_t lddz = p.lddy;
-    if (p.act != SOM_ACT_NONE && p.rows > 0) {
-        if (int rc = models_workspace(ctx, (size_t)p.rows * p.dout * sizeof(T))) return rc;
-        const int64_t groups = (p.rows * p.dout + 255) / 256;
-        hipLaunchKernelGGL(slope_kernel<T>, dim3((unsigned)(groups < 65536 ? groups : 65536)), dim3(256), 0, ctx->stream, (const T*)p.dY, p.lddy,
-                           (const T*)p.pre, p.ldpre, p.rows, p.dout, p.act, (T*)ctx->models_blob);
-        if (int rc = check_hip(ctx, hipGetLastError(), "product gradient slope launch")) return rc;
-        dz = (const T*)ctx->models_blob;
-        lddz = p.dout;
-    }
+    const bool sloped = p.act != SOM_ACT_NONE && p.rows > 0;
     ProductArgs<T> a{};
-    a.P = dz;
-    a.ldp = lddz;
     a.offsets = p.offsets;
     a.rows = (int)p.rows;
     a.K = p.K;
     a.din = p.din;
     a.dout = p.dout;
+    // workspace: dz, then the runs' sums (of the biases, then of the matrices)
+    int columns;
+    auto slopes = slope_kernel_for<T>(p.dout, columns);
+    const int64_t blocks = (p.dout + columns - 1) / columns;
+    int bias_run = run_rows(ctx, p.rows, p.K, blocks, 64);
+    if (bias_run > 256) bias_run = p.rows / 256 + p.K < 1 << 30 ? 256 : bias_run;
+    a.run = run_rows(ctx, p.rows, p.K, (int64_t)((p.dout + 255) / 256) * ((p.din + 255) / 256), 512);
+    const size_t dz_bytes = sloped ? ((size_t)p.rows * p.dout * sizeof(T) + 255) / 256 * 256 : 0;
+    const size_t bias_parts = p.dbias && p.rows > bias_run ? (size_t)run_slots(p.rows, bias_run) * p.dout : 0;
+    const size_t sum_parts = p.dA && p.rows > a.run ? (size_t)run_slots(p.rows, a.run) * p.dout * p.din : 0;
+    if (dz_bytes + bias_parts + sum_parts)
+        if (int rc = models_workspace(ctx, dz_bytes + (bias_parts > sum_parts ? bias_parts : sum_parts) * sizeof(float))) return rc;
+    T* dz = (T*)ctx->models_blob;
+    float* parts = (float*)((char*)ctx->models_blob + dz_bytes);
+    if (sloped || p.dbias) {
+        const int64_t runs = most_runs(p.rows, p.K, bias_run), y = runs < 32768 ? runs : 32768;
+        hipLaunchKernelGGL(slopes, dim3((unsigned)blocks, (unsigned)y, (unsigned)((runs + y - 1) / y)), dim3(256), 0, ctx->stream, (const T*)p.dY, p.lddy,
+                           (const T*)p.pre, p.ldpre, p.offsets, p.K, (int)p.rows, p.dout, p.act, sloped ? dz : nullptr, (T*)p.dbias, bias_run, parts);
+        if (int rc = check_hip(ctx, hipGetLastError(), "product gradient slope launch")) return rc;
+        if (bias_parts)
+            if (int rc = runs_join(ctx, p.offsets, p.K, p.rows, bias_run, parts, p.dout, (T*)p.dbias)) return rc;
+    }
+    a.P = sloped ? dz : (const T*)p.dY;
+    a.ldp = sloped ? p.dout : p.lddy;
     if (p.dX && p.rows > 0) {
         a.Q = (const T*)p.A;
         a.out = (T*)p.dX;
@@ -743,12 +877,10 @@ static int product_grad_typed(som_ctx* ctx, const NodeProductGrad& p)
         a.Q = (const T*)p.X;
         a.ldq = p.ldx;
         a.out = (T*)p.dA;
+        a.ldo = p.din;
+        a.parts = parts;
         if (int rc = product_launch<T, kOuterSums>(ctx, a, "product gradient (matrices) launch")) return rc;
-    }
-    if (p.dbias) {
-        hipLaunchKernelGGL(bias_grad_kernel<T>, dim3((unsigned)((p.dout + 63) / 64), (unsigned)p.K), dim3(256), 0, ctx->stream, dz, lddz, p.offsets,
-                           p.rows, p.dout, (T*)p.dbias);
-        if (int rc = check_hip(ctx, hipGetLastError(), "product gradient (biases) launch")) return rc;
+        if (sum_parts) return runs_join(ctx, p.offsets, p.K, p.rows, a.run, parts, (int64_t)p.dout * p.din, (T*)p.dA);
     }
     return SOM_OK;
 }

@@ -194,6 +194,20 @@ def test_product_and_gradient(som, M, K, Din, Dout, extra, lead, how, act, bias,
 
 
 @pytest.mark.parametrize("dtype", ref.TYPES)
+@pytest.mark.parametrize("M, K, Din, Dout, how, act", [(20_000, 1, 64, 48, "whole", "silu"), (30_001, 1, 9, 5, "whole", "none"), (12_345, 3, 24, 272, "one", "relu"),
+                                                      (9000, 2, 300, 16, "skew", "gelu_tanh"), (70_000, 20, 8, 8, "one", "none"), (5000, 40, 40, 33, "skew", "gelu")])
+def test_gradient_of_long_groups(som, M, K, Din, Dout, how, act, dtype):
+    """Groups whose sums over rows are taken in runs and joined."""
+    gen = torch.Generator().manual_seed(M)
+    offsets = None if how == "whole" else cut(gen, M, K, how)
+    X, A, dY, Z = (normal(gen, *s, dtype=dtype) for s in ((M, Din), (K, Dout, Din), (M, Dout), (M, Dout)))
+    got = som.som_node_product_grad(dY.cuda(), X.cuda(), A.cuda(), offsets=None if offsets is None else offsets.cuda(), pre=Z.cuda(), activation=act)
+    want = ref.product_grad(dY, X, A, offsets, Z, act, torch.zeros(M, Din, dtype=dtype))
+    for g, i, name in zip(got, (0, 2, 4), ("dX", "dA", "dbias")):
+        ref.check(g, want[i], want[i + 1], name)
+
+
+@pytest.mark.parametrize("dtype", ref.TYPES)
 def test_product_without_rows(som, dtype):
     X, A = torch.empty(0, 24, dtype=dtype, device="cuda"), torch.randn(3, 8, 24, device="cuda").to(dtype)
     offsets = torch.zeros(4, dtype=torch.int32, device="cuda")
