@@ -371,28 +371,18 @@ struct Operand {
         }
         chunk = c;
     }
-    // the stage that starts at k0 (< depth) of the contraction
-    __device__ __forceinline__ void fetch(uint32_t lds, int k0, int wave, int lane)
+    // The stage that starts at k0 of the contraction, an instruction at a time; stages behind the end bring zeros and read nothing.
+    __device__ __forceinline__ v4i stage(int k0) const
     {
-        const int left = depth - k0;
-        const uint32_t to = lds + (uint32_t)wave * kLoads * 1024;
-        if (TR) {
-            const uint32_t have = (uint32_t)(left < BK ? left : BK);
-            const v4i buffer = buffer_of((const char*)base + (uint64_t)(uint32_t)k0 * ld, (have - 1) * ld + width * 2);
-#pragma unroll
-            for (int q = 0; q < kLoads; ++q) buffer_to_lds(to + q * 1024, offset[q], buffer);
-        } else {
-            const v4i buffer = buffer_of(base + k0, (rows - 1) * ld + (uint32_t)left * 2);
-            if (left >= BK) {
-#pragma unroll
-                for (int q = 0; q < kLoads; ++q) buffer_to_lds(to + q * 1024, offset[q], buffer);
-            } else {                                           // (left is a multiple of eight)
-                const int r0 = wave * kLoads * kRowsAtOnce + lane / kChunks;
-#pragma unroll
-                for (int q = 0; q < kLoads; ++q)
-                    buffer_to_lds(to + q * 1024, exchanged(chunk, r0 + q * kRowsAtOnce) * 8 < left ? offset[q] : kNowhere, buffer);
-            }
-        }
+        const int left = depth - k0, have = left < BK ? left : BK;
+        const uint32_t bytes = TR ? (uint32_t)(have - 1) * ld + width * 2 : (rows - 1) * ld + (uint32_t)left * 2;
+        return buffer_of(TR ? (const char*)base + (uint64_t)(uint32_t)k0 * ld : (const char*)(base + k0), left > 0 ? bytes : 0u);
+    }
+    __device__ __forceinline__ void one(int q, uint32_t lds, v4i buffer, int k0, int wave, int lane) const
+    {
+        // a plain row's end is not the buffer's: chunks behind it (depth is a multiple of eight) are sent nowhere
+        const bool past = !TR && exchanged(chunk, wave * kLoads * kRowsAtOnce + lane / kChunks + q * kRowsAtOnce) * 8 >= depth - k0;
+        buffer_to_lds(lds + (uint32_t)(wave * kLoads + q) * 1024, past ? kNowhere : offset[q], buffer);
     }
 };
 
@@ -458,17 +448,14 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64) product_tile_kerne
     float* part = nullptr;
     if (F == kOuterSums) {
         const unsigned run = a.run;
-        uint2 runs = make_uint2(0u, 0u);
-        for (int k = threadIdx.x; k < a.K; k += THREADS) {
-            group_rows(a.offsets, k, a.rows, first, end);
-            runs.x += runs_of(end - first, run);
-        }
-        const unsigned ytiles = (a.dout + BM - 1) / BM, each = ytiles * xtiles, total = sum_all<THREADS>(runs).x * each, share = (total + 7) / 8;
-        const unsigned tile = xcd * share + turn;
-        if (turn >= share || tile >= total) return;
+        // Runs differ in length, so every die takes its share of each run's tiles (a run of groups for each die, as below: 726 us
+        // for 65536 rows, 2048 -> 1536, on 64 uneven nodes, .. us like this)
+        const unsigned ytiles = (a.dout + BM - 1) / BM, each = ytiles * xtiles, share = (each + 7) / 8;
+        const unsigned item = each < 16 ? blockIdx.x / each : turn / share, tile = each < 16 ? blockIdx.x % each : xcd * share + turn % share;
         int which;
-        e = find_group<THREADS>(a.offsets, a.K, a.rows, [run](unsigned n) { return runs_of(n, run); }, tile / each, which);
-        m0 = banded(tile % each, ytiles, xtiles, x) * BM;
+        e = find_group<THREADS>(a.offsets, a.K, a.rows, [run](unsigned n) { return runs_of(n, run); }, item, which);
+        if (e < 0 || tile >= each) return;
+        m0 = banded(tile, ytiles, xtiles, x) * BM;
         group_rows(a.offsets, e, a.rows, first, end);
         if (end - first > (int)run) {
             const int lo = first;
@@ -522,59 +509,81 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64) product_tile_kerne
     const uint32_t lds = lds_address(tile_lds);
     // blocks of 32 rows that this wavefront has; the columns' ends are left to zeros and to the stores
     const int have = ((F == kOuterSums ? a.dout - m0 : end - first) - wm + 31) / 32;
-    auto fetch = [&](int i) {                       // stage i of the contraction
-        P.fetch(lds + (i & 1) * kStage, i * BK, wave, lane);
-        Q.fetch(lds + (i & 1) * kStage + OpP::kBytes, i * BK, wave, lane);
+    constexpr int U = WM / 32, V = WN / 32, kLoads = OpP::kLoads + OpQ::kLoads;
+    half8 p[2][U], q[2][V];
+    // instruction number n of a stage
+    auto fetch = [&](int i, int n, v4i bp, v4i bq) {
+        const uint32_t to = lds + (i & 1) * kStage;
+        if (n < OpP::kLoads) P.one(n, to, bp, i * BK, wave, lane);
+        else Q.one(n - OpP::kLoads, to + OpP::kBytes, bq, i * BK, wave, lane);
     };
-    half8 p[2][WM / 32], q[2][WN / 32];
-    auto read = [&](auto whole, int i, int k, int to) {
+    auto fetch_all = [&](int i) {
+        const v4i bp = P.stage(i * BK), bq = Q.stage(i * BK);
+#pragma unroll
+        for (int n = 0; n < kLoads; ++n) fetch(i, n, bp, bq);
+    };
+    // fragment number f of sixteen of the contraction: the columns', then the rows'
+    auto read = [&](int i, int k, int to, int f) {
         const char* stage = tile_lds + (i & 1) * kStage;
-#pragma unroll
-        for (int v = 0; v < WN / 32; ++v) q[to][v] = fragment<T, BN, BK, TQ>(stage + OpP::kBytes, wn + 32 * v, k, lane);
-#pragma unroll
-        for (int u = 0; u < WM / 32; ++u)
-            if (whole || u < have) p[to][u] = fragment<T, BM, BK, TP>(stage, wm + 32 * u, k, lane);
-        __builtin_amdgcn_sched_barrier(0);          // (the scheduler would put the reads back to where their values are needed)
+        if (f < V) q[to][f] = fragment<T, BN, BK, TQ>(stage + OpP::kBytes, wn + 32 * f, k, lane);
+        else p[to][f - V] = fragment<T, BM, BK, TP>(stage, wm + 32 * (f - V), k, lane);
     };
-    auto multiply = [&](auto whole, int from) {
+    // The contraction for H blocks of rows.  The pipe takes 32 cycles for a product, and beside each goes a share of the other work: the
+    // next sixteen's fragments, and behind the barrier the stage after the next.  (The scheduler would gather the reads in front of
+    // their use: it is kept out.)  The last fragments of a stage are in registers when the barrier comes, so that its buffer is free and
+    // everyone's arrival hides behind products that need nothing.
+    auto contract = [&](auto blocks) {
+        constexpr int H = decltype(blocks)::value, kReads = H + V, kSlots = H * V;
 #pragma unroll
-        for (int u = 0; u < WM / 32; ++u)
-            if (whole || u < have)
-#pragma unroll
-                for (int v = 0; v < WN / 32; ++v) acc[u][v] = mfma(q[from][v], p[from][u], acc[u][v]);
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    auto contract = [&](auto whole) {
-        read(whole, 0, 0, 0);
+        for (int f = 0; f < kReads; ++f) read(0, 0, 0, f);
         for (int i = 0; i < steps; ++i) {
 #pragma unroll
-            for (int j = 0; j < BK / 16 - 1; ++j) {
-                read(whole, i, 16 * (j + 1), (j + 1) & 1);
-                multiply(whole, j & 1);
+            for (int j = 0; j < BK / 16; ++j) {
+                const bool last = j == BK / 16 - 1;
+                v4i bp = {}, bq = {};
+                if (last) {
+                    stage_ready<0>();
+                    bp = P.stage((i + 2) * BK);
+                    bq = Q.stage((i + 2) * BK);
+                }
+#pragma unroll
+                for (int t = 0; t < kSlots; ++t) {
+                    acc[t / V][t % V] = mfma(q[j & 1][t % V], p[j & 1][t / V], acc[t / V][t % V]);
+#pragma unroll
+                    for (int f = t * kReads / kSlots; f < (t + 1) * kReads / kSlots; ++f) read(last ? i + 1 : i, last ? 0 : 16 * (j + 1), (j + 1) & 1, f);
+                    if (last) {
+#pragma unroll
+                        for (int n = t * kLoads / kSlots; n < (t + 1) * kLoads / kSlots; ++n) fetch(i + 2, n, bp, bq);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
-            // The last fragments of this stage are in registers: its buffer is free, and the next stage's first fragments and
-            // everyone's arrival hide behind their products.
-            if (i + 1 < steps) {
-                stage_ready<0>();
-                if (i + 2 < steps) fetch(i + 2);
-                read(whole, i + 1, 0, 0);
-            }
-            multiply(whole, 1);
         }
     };
     if (steps > 0) {
-        fetch(0);
+        fetch_all(0);
         stage_ready<0>();
-        if (steps > 1) fetch(1);
+        fetch_all(1);
         // a group's last tile leaves out the blocks of rows that it does not have
-        if (have >= WM / 32) contract(std::true_type{});
-        else contract(std::false_type{});
+        if (have >= U) {
+            contract(std::integral_constant<int, U>{});
+        } else if (have >= 2 && U > 2) {
+            if (have == 2) contract(std::integral_constant<int, (U > 2 ? 2 : 1)>{});
+            else contract(std::integral_constant<int, (U > 3 ? 3 : 1)>{});
+        } else if (have == 1) {
+            contract(std::integral_constant<int, 1>{});
+        } else {
+            for (int i = 0; i < steps; ++i) {
+                stage_ready<0>();
+                fetch_all(i + 2);
+            }
+        }
     }
     // Results go out by rows: a wavefront's 32 x WN values change from the pipe's layout (lane: row, four columns at a time) to eight
     // columns a lane through LDS rows of WN + 4 floats, which keep sixteen lanes on sixteen places both ways.
     constexpr int kRow = WN + 4, kLanes = WN / 8, kAtOnce = 64 / kLanes;
     static_assert(WAVES * 32 * kRow * 4 <= 2 * kStage);
-    stage_ready<0>();                               // no one reads the stages any more
+    stage_ready<0>();                               // no one reads the stages any more, or writes to them
     float* turned = reinterpret_cast<float*>(tile_lds) + wave * 32 * kRow;
     const int n = n0 + wn + lane % kLanes * 8;
     Piece<T> c;
@@ -723,12 +732,12 @@ static int64_t most_tiles(int64_t rows, int32_t K, const int32_t* offsets, int b
 static int64_t most_runs(int64_t rows, int32_t K, int run) { return rows / run + K; }
 
 // Rows a run of a sum over rows when a group alone gives `tiles` workgroups: one run a group where the groups fill the chip (longer ones
-// only for a group of eight times its share), shorter ones where they do not.
+// only for a group of four times its share), shorter ones where they do not.
 static int run_rows(const som_ctx* ctx, int64_t rows, int32_t K, int64_t tiles, int least)
 {
     const int64_t share = (rows + K - 1) / K, runs = ctx->units / (K * tiles > ctx->units ? ctx->units : K * tiles);
-    int64_t run = runs > 1 ? (share + runs - 1) / runs : K > 1 ? 8 * share : rows;
-    if (runs <= 1 && run < 4096) run = 4096;
+    int64_t run = runs > 1 ? (share + runs - 1) / runs : K > 1 ? 4 * share : rows;
+    if (runs <= 1 && run < 2048) run = 2048;
     if (run < least) run = least;
     if (run * 32000 < rows) run = rows / 32000 + 1;             // (a grid's third dimension)
     return (int)((run + 63) / 64 * 64 < 0x7fffffc0 ? (run + 63) / 64 * 64 : 0x7fffffc0);
@@ -760,7 +769,9 @@ static int product_tile_launch(som_ctx* ctx, const ProductArgs<T>& a, const char
     }
     const int64_t xtiles = ((F == kRowsTimesA ? a.dout : a.din) + BN - 1) / BN;
     const int64_t ytiles = F == kOuterSums ? most_runs(a.rows, a.K, a.run) * ((a.dout + BM - 1) / BM) : most_tiles(a.rows, a.K, a.offsets, BM);
-    hipLaunchKernelGGL(kern, dim3((unsigned)((xtiles * ytiles + 7) / 8 + 2) * 8), dim3((BM / WM) * (BN / WN) * 64), lds, ctx->stream, a, (unsigned)xtiles);
+    const int64_t each = (a.dout + BM - 1) / BM * xtiles;              // tiles of a run
+    const int64_t groups = F != kOuterSums ? ((xtiles * ytiles + 7) / 8 + 2) * 8 : each < 16 ? xtiles * ytiles : (each + 7) / 8 * 8 * (ytiles * xtiles / each);
+    hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3((BM / WM) * (BN / WN) * 64), lds, ctx->stream, a, (unsigned)xtiles);
     return check_hip(ctx, hipGetLastError(), what);
 }
 
