@@ -276,6 +276,7 @@ struct Operand {
     int depth;                 // of the contraction
     int rows;                  // rows (TR: values in a row) that exist, counted from base
     int64_t ld;                // values
+    bool brief;                // a row of the matrix has fewer values than a chunk
     int chunk, row;            // the LDS chunk and row that this lane fills first
     uint32_t offset[kLoads];   // ALIGNED: in bytes from a stage's first row
 
@@ -286,11 +287,12 @@ struct Operand {
         if (sizeof(T) == 4) return c ^ ((r & 4) << 1);
         return R >= 128 ? c ^ ((r & 3) << 2) : c ^ ((r & 2) << 1);
     }
-    __device__ __forceinline__ void init(const T* b, int d, int exist, int64_t stride, int wave, int lane)
+    __device__ __forceinline__ void init(const T* b, int d, int exist, int64_t stride, int values, int wave, int lane)
     {
         static_assert(kLoads >= 1 && kBytes % (1024 * WAVES) == 0 && 64 % kChunks == 0);
         base = b;
         depth = d;
+        brief = values < E;
         rows = exist < R ? exist : R;
         ld = stride;
         chunk = lane % kChunks;
@@ -315,23 +317,45 @@ struct Operand {
         const bool past = !TR && exchanged(chunk, row + q * kRowsAtOnce) * E >= depth - k0;
         buffer_to_lds(lds + (uint32_t)(wave * kLoads + q) * 1024, past ? kNowhere : offset[q], buffer);
     }
-    __device__ __forceinline__ Piece<T> load(int q, int k0) const
+    // values of this lane's chunk that exist (E at most: all of it)
+    __device__ __forceinline__ int left(int q, int k0) const
     {
         const int r = row + q * kRowsAtOnce, from = exchanged(chunk, r) * E;
-        const int left = TR ? (k0 + r < depth ? rows - from : 0) : (r < rows ? depth - k0 - from : 0);
+        const int n = TR ? (k0 + r < depth ? rows - from : 0) : (r < rows ? depth - k0 - from : 0);
+        return n < E ? n : E;
+    }
+    // A chunk at a row's end is read as the row's last sixteen bytes and moved down by `store`, which is where it is waited for.
+    __device__ __forceinline__ v4i load(int q, int k0) const
+    {
+        typedef int any4 __attribute__((ext_vector_type(4), aligned(2)));
+        const int r = row + q * kRowsAtOnce, from = exchanged(chunk, r) * E, n = left(q, k0);
         const T* p = TR ? base + (k0 + r) * ld + from : base + r * ld + k0 + from;
-        Piece<T> x;
-        if (left >= E) {
-            x.load(p);
-        } else {
+        v4i x = {};
+        if (brief) {
 #pragma unroll
-            for (int j = 0; j < E; ++j) x.e[j] = j < left ? p[j] : (T)0.0f;
+            for (int j = 0; j < E; ++j) {
+                if (j >= n) continue;
+                if constexpr (sizeof(T) == 4) x[j] = __builtin_bit_cast(int, p[j]);
+                else x[j / 2] |= (int)__builtin_bit_cast(uint16_t, p[j]) << (j % 2 * 16);
+            }
+        } else if (n > 0) {
+            x = *reinterpret_cast<const any4*>(p - (E - n));
         }
         return x;
     }
-    __device__ __forceinline__ void store(int q, char* stage, const Piece<T>& x, int wave, int lane) const
+    __device__ __forceinline__ void store(int q, int k0, char* stage, v4i x, int wave, int lane) const
     {
-        *reinterpret_cast<typename Fragment<T>::type*>(stage + (wave * kLoads + q) * 1024 + lane * 16) = __builtin_bit_cast(typename Fragment<T>::type, x);
+        const int n = left(q, k0);
+        if (n < E && !brief) {
+            const int s = 8 * (int)sizeof(T) * (E - n);                      // 16 .. 112 bits, more for a chunk of which nothing exists
+            const uint64_t lo = (uint32_t)x[0] | (uint64_t)(uint32_t)x[1] << 32, hi = (uint32_t)x[2] | (uint64_t)(uint32_t)x[3] << 32;
+            const uint64_t lo2 = n <= 0 ? 0u : s < 64 ? lo >> s | hi << (64 - s) : hi >> (s - 64), hi2 = n <= 0 || s >= 64 ? 0u : hi >> s;
+            x[0] = (int)lo2;
+            x[1] = (int)(lo2 >> 32);
+            x[2] = (int)hi2;
+            x[3] = (int)(hi2 >> 32);
+        }
+        *reinterpret_cast<v4i*>(stage + (wave * kLoads + q) * 1024 + lane * 16) = x;
     }
 };
 
@@ -452,12 +476,12 @@ __global__ void __launch_bounds__(Tile<B>::THREADS) product_tile_kernel(ProductA
     OpQ Q;
     const int depth = F == kRowsTimesA ? a.din : F == kRowsTimesAt ? a.dout : end - first;
     if (F == kOuterSums) {
-        P.init(a.P + (int64_t)first * a.ldp + m0, depth, a.dout - m0, a.ldp, wave, lane);
-        Q.init(a.Q + (int64_t)first * a.ldq + n0, depth, a.din - n0, a.ldq, wave, lane);
+        P.init(a.P + (int64_t)first * a.ldp + m0, depth, a.dout - m0, a.ldp, a.dout, wave, lane);
+        Q.init(a.Q + (int64_t)first * a.ldq + n0, depth, a.din - n0, a.ldq, a.din, wave, lane);
     } else {
-        P.init(a.P + (int64_t)first * a.ldp, depth, end - first, a.ldp, wave, lane);
+        P.init(a.P + (int64_t)first * a.ldp, depth, end - first, a.ldp, depth, wave, lane);
         const T* A = a.Q + (int64_t)e * a.dout * a.din;
-        Q.init(F == kRowsTimesA ? A + (int64_t)n0 * a.din : A + n0, depth, Nn - n0, a.din, wave, lane);
+        Q.init(F == kRowsTimesA ? A + (int64_t)n0 * a.din : A + n0, depth, Nn - n0, a.din, a.din, wave, lane);
     }
     f32x16 acc[WM / 32][WN / 32] = {};
     const int steps = (depth + BK - 1) / BK;
@@ -466,20 +490,20 @@ __global__ void __launch_bounds__(Tile<B>::THREADS) product_tile_kernel(ProductA
     const int have = ((F == kOuterSums ? a.dout - m0 : end - first) - wm + 31) / 32;
     constexpr int U = WM / 32, V = WN / 32, kLoads = OpP::kLoads + OpQ::kLoads;
     Frag p[2][U], q[2][V];
-    Piece<T> held[ALIGNED ? 1 : kLoads];            // a stage on its way through registers
+    v4i held[ALIGNED ? 1 : kLoads];                 // a stage on its way through registers
     // instruction number n of a stage
-    auto fetch = [&](int i, int n, v4i bp, v4i bq) {
+    auto fetch = [&](int i, int n, v4i bp, v4i bq) __attribute__((always_inline)) {
         const uint32_t to = lds + (i & 1) * kStage;
         if (n < OpP::kLoads) P.one(n, to, bp, i * BK, wave);
         else Q.one(n - OpP::kLoads, to + OpP::kBytes, bq, i * BK, wave);
     };
-    auto load = [&](int i, int n) { held[n] = n < OpP::kLoads ? P.load(n, i * BK) : Q.load(n - OpP::kLoads, i * BK); };
-    auto store = [&](int i, int n) {
+    auto load = [&](int i, int n) __attribute__((always_inline)) { held[n] = n < OpP::kLoads ? P.load(n, i * BK) : Q.load(n - OpP::kLoads, i * BK); };
+    auto store = [&](int i, int n) __attribute__((always_inline)) {
         char* to = tile_lds + (i & 1) * kStage;
-        if (n < OpP::kLoads) P.store(n, to, held[n], wave, lane);
-        else Q.store(n - OpP::kLoads, to + OpP::kBytes, held[n], wave, lane);
+        if (n < OpP::kLoads) P.store(n, i * BK, to, held[n], wave, lane);
+        else Q.store(n - OpP::kLoads, i * BK, to + OpP::kBytes, held[n], wave, lane);
     };
-    auto fetch_all = [&](int i) {
+    auto fetch_all = [&](int i) __attribute__((always_inline)) {
         if constexpr (ALIGNED) {
             const v4i bp = P.stage(i * BK), bq = Q.stage(i * BK);
 #pragma unroll
@@ -492,7 +516,7 @@ __global__ void __launch_bounds__(Tile<B>::THREADS) product_tile_kernel(ProductA
         }
     };
     // fragment number f of a step: the columns', then the rows'
-    auto read = [&](int i, int j, int to, int f) {
+    auto read = [&](int i, int j, int to, int f) __attribute__((always_inline)) {
         const char* stage = tile_lds + (i & 1) * kStage;
         if (f < V) q[to][f] = fragment<T, BN, TQ>(stage + OpP::kBytes, wn + 32 * f, j, lane);
         else p[to][f - V] = fragment<T, BM, TP>(stage, wm + 32 * (f - V), j, lane);
@@ -501,7 +525,7 @@ __global__ void __launch_bounds__(Tile<B>::THREADS) product_tile_kernel(ProductA
     // next step's fragments, and behind the barrier the stage after the next.  (The scheduler would gather the reads in front of
     // their use: it is kept out.)  The last fragments of a stage are in registers when the barrier comes, so that its buffer is free and
     // everyone's arrival hides behind products that need nothing.
-    auto contract = [&](auto blocks) {
+    auto contract = [&](auto blocks) __attribute__((always_inline)) {
         constexpr int H = decltype(blocks)::value, kReads = H + V, kSlots = H * V;
 #pragma unroll
         for (int f = 0; f < kReads; ++f) read(0, 0, 0, f);
@@ -574,13 +598,13 @@ __global__ void __launch_bounds__(Tile<B>::THREADS) product_tile_kernel(ProductA
     typedef Piece<T, 8> Eight;
     constexpr bool kWhole = ALIGNED && sizeof(T) == 2;
     const int left = Nn - n;
-    auto load8 = [&](Eight& x, const T* from) {
+    auto load8 = [&](Eight& x, const T* from) __attribute__((always_inline)) {
         if (kWhole || left >= 8) x.load(from);
         else
 #pragma unroll
             for (int j = 0; j < 8; ++j) x.e[j] = j < left ? from[j] : (T)0.0f;
     };
-    auto store8 = [&](const Eight& x, T* to) {
+    auto store8 = [&](const Eight& x, T* to) __attribute__((always_inline)) {
         if (kWhole || left >= 8) x.store(to);
         else
 #pragma unroll
