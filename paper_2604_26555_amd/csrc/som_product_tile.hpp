@@ -924,8 +924,8 @@ static int runs_join(som_ctx* ctx, const int32_t* offsets, int32_t K, int64_t ro
         hipLaunchKernelGGL((runs_join_kernel<T, 16>), dim3((unsigned)((count + 63) / 64), (unsigned)y), dim3(1024), 0, ctx->stream, offsets, K, (int)rows,
                            run, parts, count, out);
     } else {
-        const int64_t blocks = (count + 255) / 256;
-        hipLaunchKernelGGL((runs_join_kernel<T, 1>), dim3((unsigned)(blocks < 4096 ? blocks : 4096), (unsigned)y), dim3(256), 0, ctx->stream, offsets, K,
+        const int64_t blocks = (count + 255) / 256, share = 16 * ctx->units / y + 1;       // (most of the y find no group)
+        hipLaunchKernelGGL((runs_join_kernel<T, 1>), dim3((unsigned)(blocks < share ? blocks : share), (unsigned)y), dim3(256), 0, ctx->stream, offsets, K,
                            (int)rows, run, parts, count, out);
     }
     return check_hip(ctx, hipGetLastError(), "product gradient join launch");

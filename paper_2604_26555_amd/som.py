@@ -153,6 +153,9 @@ def _matrix(t: torch.Tensor, name: str):
     return rows, columns, ld if rows > 1 else max(columns, ld)
 
 
+# address of the current stream: without making a Stream object (2 us) where torch has a way to
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
 _ROWS = {torch.float32: SOM_ROWS_FLOAT, torch.bfloat16: SOM_ROWS_BFLOAT, torch.float16: SOM_ROWS_HALF}
 _ACTIVATIONS = {"none": SOM_ACT_NONE, "relu": SOM_ACT_RELU, "silu": SOM_ACT_SILU, "gelu": SOM_ACT_GELU, "gelu_tanh": SOM_ACT_GELU_TANH}
 
@@ -197,6 +200,7 @@ class Som:
         if rc != SOM_OK:
             raise SomError(rc, "som_create", self.lib.som_strerror(rc).decode())
         self._h = handle
+        self._raw = self.stream.cuda_stream
 
     def close(self):
         if getattr(self, "_h", None):
@@ -374,7 +378,7 @@ class Som:
     # ------------------------------------------------------------------ local models: one matrix per node
     def _empty(self, shape, dtype):
         """A new tensor that this context's stream may write at once: its memory comes from that stream's pool."""
-        if torch.cuda.current_stream(self.device) == self.stream:
+        if _raw_stream(self.device.index) == self._raw:
             return torch.empty(shape, dtype=dtype, device=self.device)
         with torch.cuda.stream(self.stream):
             return torch.empty(shape, dtype=dtype, device=self.device)

@@ -115,12 +115,20 @@ def test_null_context(stub):
 
 def test_without_memory_for_the_workspace(ctx):
     ctx.limit(16)
-    rc, kernels = call(ctx, "som_group")
+    rc, kernels = call(ctx, "som_group", T=100_000)
     assert rc == -2 and kernels == [] and "workspace" in ctx.error()
     rc, kernels = call(ctx, "som_node_product_grad")
     assert rc == -2 and kernels == []
     ctx.limit()
-    assert call(ctx, "som_group")[0] == SOM_OK
+    assert call(ctx, "som_group", T=100_000)[0] == SOM_OK
+
+
+@pytest.mark.parametrize("T, k, K, launches", [(1, 8, 128, 1), (8192, 2, 64, 1), (8193, 2, 64, 3), (100, 1, 8205, 1), (100, 1, 8300, 4), (50_000, 1, 2047, 3),
+                                               (50_000, 1, 2048, 4), (50_000, 1, 32768, 4)])
+def test_group_routes(ctx, T, k, K, launches):
+    """One launch up to 16384 pairs (where four wavefronts' counters fit LDS), beyond it three up to 2047 nodes and four above."""
+    rc, kernels = call(ctx, "som_group", T=T, k=k, K=K)
+    assert rc == SOM_OK and len(kernels) == launches, kernels
 
 
 def test_a_failed_launch_is_reported(ctx):
