@@ -36,7 +36,7 @@ __device__ __forceinline__ uint64_t lanes_alike(int b, int bits)
 }
 
 // The chip's eight dies take workgroups in turn; each gets a run of them, so that lines which neighbours share are written whole from one
-// die's cache.  (1,000,000 rows of 50 floats to 1024 nodes: dispatch 107 us in turn, .. in runs.)
+// die's cache.  (1,000,000 rows of 50 floats to 1024 nodes: dispatch 107 us in turn, 77 in runs.)
 __device__ __forceinline__ int64_t run_of_die(unsigned groups) { return (int64_t)(blockIdx.x % 8) * ((groups + 7) / 8) + blockIdx.x / 8; }
 
 // Exclusive sums over the threads of a workgroup.
@@ -82,7 +82,7 @@ __device__ __forceinline__ void scatter_pairs(const int32_t* __restrict__ node, 
 }
 
 // Few pairs: one workgroup of 16 wavefronts, `waves` of which have counters (and pairs).  What it takes is latency: a row's eight pairs and
-// 128 nodes .. us, 16384 pairs and 64 nodes .. us, where the four kernels below take 29 and 32.
+// 128 nodes 4 us on the GPU, and 36 us with the four launches that larger calls had.
 __global__ void __launch_bounds__(1024) group_small_kernel(const int32_t* __restrict__ node, int pairs, int K, int waves, int32_t* __restrict__ offsets,
                                                            int32_t* __restrict__ order, int32_t* __restrict__ slot)
 {
@@ -223,23 +223,26 @@ __global__ void __launch_bounds__(256) group_scatter_kernel(const int32_t* __res
     scatter_pairs(node, lo, hi, K, place, order, slot);
 }
 
-// Workgroups for `items` rows or pairs, `each` of them a workgroup at a time, in eights: a grid holds fewer than 2^32 work-items.
+// Workgroups for `items` rows or pairs, `each` of them a workgroup at a time and `across` workgroups for each, in eights: a grid holds fewer
+// than 2^32 work-items.
 static dim3 row_grid(int64_t items, int each, int64_t across = 1)
 {
-    const int64_t groups = ((items + each - 1) / each + 7) / 8 * 8, most = 1 << 23;
-    return dim3((unsigned)(groups < most ? groups : most), (unsigned)across);
+    const int64_t groups = ((items + each - 1) / each + 7) / 8 * 8, most = (1 << 23) / across / 8 * 8;
+    return dim3((unsigned)((groups < most ? groups : most) * across));
 }
 
-// A lane per piece of a row; LANES of them and gridDim.y workgroups share a row.
+// A lane per piece of a row; LANES of them and `across` neighbouring workgroups share a row (with a row's parts in different corners of the grid
+// 16384 rows of 2048 bf16 to four nodes: sorted 91 us, 75 like this; combined 83 and 70).
 template <class T, int LANES>
 __global__ void __launch_bounds__(256) dispatch_kernel(const T* __restrict__ X, int64_t rows, int D, int64_t ldx, const int32_t* __restrict__ slot, int k,
-                                                       const float* __restrict__ weight, T* __restrict__ Y, int64_t places, int64_t ldy)
+                                                       const float* __restrict__ weight, T* __restrict__ Y, int64_t places, int64_t ldy, unsigned across)
 {
     constexpr int N = Piece<T>::N;
-    const int c = blockIdx.y * LANES + threadIdx.x % LANES;
+    const unsigned group = (unsigned)run_of_die(gridDim.x);
+    const int c = group % across * LANES + threadIdx.x % LANES;
     if (c * N >= D) return;
     const int64_t at = piece_at<T>(c, D);
-    for (int64_t t = run_of_die(gridDim.x) * (256 / LANES) + threadIdx.x / LANES; t < rows; t += (int64_t)gridDim.x * (256 / LANES)) {
+    for (int64_t t = (int64_t)(group / across) * (256 / LANES) + threadIdx.x / LANES; t < rows; t += (int64_t)(gridDim.x / across) * (256 / LANES)) {
         Piece<T> x;
         x.load(X + t * ldx + at);
         for (int j0 = 0; j0 < k; j0 += 4) {
@@ -266,13 +269,14 @@ __global__ void __launch_bounds__(256) dispatch_kernel(const T* __restrict__ X, 
 
 template <class T, int LANES>
 __global__ void __launch_bounds__(256) combine_kernel(const T* __restrict__ Y, int64_t places, int D, int64_t ldy, const int32_t* __restrict__ slot,
-                                                      int64_t rows, int k, const float* __restrict__ weight, T* __restrict__ out, int64_t ldo)
+                                                      int64_t rows, int k, const float* __restrict__ weight, T* __restrict__ out, int64_t ldo, unsigned across)
 {
     constexpr int N = Piece<T>::N;
-    const int c = blockIdx.y * LANES + threadIdx.x % LANES;
+    const unsigned group = (unsigned)run_of_die(gridDim.x);
+    const int c = group % across * LANES + threadIdx.x % LANES;
     if (c * N >= D) return;
     const int64_t at = piece_at<T>(c, D);
-    for (int64_t t = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES; t < rows; t += (int64_t)gridDim.x * (256 / LANES)) {
+    for (int64_t t = (int64_t)(group / across) * (256 / LANES) + threadIdx.x / LANES; t < rows; t += (int64_t)(gridDim.x / across) * (256 / LANES)) {
         float sum[N];
 #pragma unroll
         for (int e = 0; e < N; ++e) sum[e] = 0.0f;
@@ -468,7 +472,7 @@ static int dispatch_typed(som_ctx* ctx, const T* X, int64_t rows, int32_t D, int
     } else {
         const int pieces = (D + Piece<T>::N - 1) / Piece<T>::N, lanes = row_lanes(pieces, 64);
         hipLaunchKernelGGL(SOM_ROW_KERNELS(dispatch_kernel, T), row_grid(rows, 256 / lanes, (pieces + lanes - 1) / lanes), dim3(256), 0, ctx->stream, X,
-                           rows, D, ldx, slot, k, weight, Y, places, ldy);
+                           rows, D, ldx, slot, k, weight, Y, places, ldy, (unsigned)((pieces + lanes - 1) / lanes));
     }
     return check_hip(ctx, hipGetLastError(), "dispatch launch");
 }
@@ -483,7 +487,7 @@ static int combine_typed(som_ctx* ctx, const T* Y, int64_t places, int32_t D, in
     } else {
         const int pieces = (D + Piece<T>::N - 1) / Piece<T>::N, lanes = row_lanes(pieces, 64);
         hipLaunchKernelGGL(SOM_ROW_KERNELS(combine_kernel, T), row_grid(rows, 256 / lanes, (pieces + lanes - 1) / lanes), dim3(256), 0, ctx->stream, Y,
-                           places, D, ldy, slot, rows, k, weight, out, ldo);
+                           places, D, ldy, slot, rows, k, weight, out, ldo, (unsigned)((pieces + lanes - 1) / lanes));
     }
     return check_hip(ctx, hipGetLastError(), "combine launch");
 }
