@@ -1,4 +1,4 @@
-// Products with the nodes' matrices: the element type's own kernels (som_product_tile.hpp), which are compiled one type a unit.
+// Products with the nodes' matrices: the element type's own kernels (som_product_tile.hpp, som_product_narrow.hpp, som_product_launch.hpp), which are compiled one type a unit.
 #include "som_internal.hpp"
 
 namespace som {

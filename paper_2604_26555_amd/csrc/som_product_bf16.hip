@@ -1,4 +1,4 @@
-#include "som_product_tile.hpp"
+#include "som_product_launch.hpp"
 
 namespace som {
 

@@ -111,10 +111,17 @@ struct Math {
     }
 };
 
-template <class T>
-__device__ __forceinline__ float activate(float z, int act)
+template <class T, int N>
+__device__ __forceinline__ void activate(float (&x)[N], int act)
 {
-    return Math<sizeof(T) == 4>::activate(z, act);
+    auto all = [&](int which) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] = Math<sizeof(T) == 4>::activate(x[j], which);
+    };
+    if (act == SOM_ACT_SILU) all(SOM_ACT_SILU);
+    else if (act == SOM_ACT_GELU) all(SOM_ACT_GELU);
+    else if (act == SOM_ACT_GELU_TANH) all(SOM_ACT_GELU_TANH);
+    else if (act == SOM_ACT_RELU) all(SOM_ACT_RELU);
 }
 
 // Rows [lo, hi) of group e, inside [0, rows) whatever the offsets hold.
@@ -437,7 +444,7 @@ __global__ void __launch_bounds__(Tile<B>::THREADS) product_tile_kernel(ProductA
     if (F == kOuterSums) {
         const unsigned run = a.run;
         // Runs differ in length, so every die takes its share of each run's tiles (a run of groups for each die, as below: 726 us
-        // for 65536 rows, 2048 -> 1536, on 64 uneven nodes, .. us like this)
+        // for 65536 rows, 2048 -> 1536, on 64 uneven nodes, 535 us like this)
         const unsigned ytiles = (a.dout + BM - 1) / BM, each = ytiles * xtiles, share = (each + 7) / 8;
         const unsigned item = each < 16 ? blockIdx.x / each : turn / share, tile = each < 16 ? blockIdx.x % each : xcd * share + turn % share;
         int which;
@@ -647,19 +654,7 @@ __global__ void __launch_bounds__(Tile<B>::THREADS) product_tile_kernel(ProductA
                     for (int j = 0; j < 8; ++j) z.e[j] = (T)x[j];
                     store8(z, a.pre + row * a.ldpre + n);
                 }
-                if (a.act == SOM_ACT_SILU) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) x[j] = activate<T>(x[j], SOM_ACT_SILU);
-                } else if (a.act == SOM_ACT_GELU) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) x[j] = activate<T>(x[j], SOM_ACT_GELU);
-                } else if (a.act == SOM_ACT_GELU_TANH) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) x[j] = activate<T>(x[j], SOM_ACT_GELU_TANH);
-                } else if (a.act == SOM_ACT_RELU) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) x[j] = activate<T>(x[j], SOM_ACT_RELU);
-                }
+                activate<T>(x, a.act);
                 if (a.residual)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) x[j] += (float)d.e[j];
@@ -786,200 +781,6 @@ __global__ void __launch_bounds__(SHARES == 1 ? 256 : 64 * SHARES) runs_join_ker
         }
         if (share == 0 && i < count) out[(int64_t)e * count + i] = (T)s;
     }
-}
-
-// Tiles of `bm` rows that the groups can have together.
-static int64_t most_tiles(int64_t rows, int32_t K, const int32_t* offsets, int bm)
-{
-    const int64_t full = (rows + bm - 1) / bm;
-    return offsets ? full + (K < rows ? K : rows) : full;
-}
-
-// Runs of `run` rows that the groups can have together.
-static int64_t most_runs(int64_t rows, int32_t K, int run) { return rows / run + K; }
-
-// Rows a run of a sum over rows when a group alone gives `tiles` workgroups: one run a group where the groups fill the chip (longer ones
-// only for a group of four times its share), shorter ones where they do not.
-static int run_rows(const som_ctx* ctx, int64_t rows, int32_t K, int64_t tiles, int least)
-{
-    const int64_t share = (rows + K - 1) / K, runs = ctx->units / (K * tiles > ctx->units ? ctx->units : K * tiles);
-    int64_t run = runs > 1 ? (share + runs - 1) / runs : K > 1 ? 4 * share : rows;
-    if (runs <= 1 && run < 2048) run = 2048;
-    if (run < least) run = least;
-    if (run * 32000 < rows) run = rows / 32000 + 1;             // (a grid's third dimension)
-    return (int)((run + 63) / 64 * 64 < 0x7fffffc0 ? (run + 63) / 64 * 64 : 0x7fffffc0);
-}
-
-static bool sixteen(const void* p) { return (uintptr_t)p % 16 == 0; }
-
-// Every row of every matrix starts at a multiple of sixteen bytes and holds whole chunks of them.
-template <class T>
-static bool product_aligned(const ProductArgs<T>& a)
-{
-    constexpr int E = 16 / sizeof(T);
-    return a.din % E == 0 && a.dout % E == 0 && a.ldp % E == 0 && a.ldq % E == 0 && a.ldo % E == 0 && a.ldr % E == 0 && a.ldpre % E == 0 && sixteen(a.P) &&
-           sixteen(a.Q) && sixteen(a.out) && sixteen(a.bias) && sixteen(a.residual) && sixteen(a.pre);
-}
-
-template <class T, Form F, int B, bool ALIGNED>
-static int product_tile_launch(som_ctx* ctx, const ProductArgs<T>& a, const char* what)
-{
-    static bool attr_set_dev[kMaxDevices] = {};
-    bool& attr_set = attr_set_dev[ctx->device];
-    auto kern = product_tile_kernel<T, F, B, ALIGNED>;
-    if (!attr_set) {
-        if (int rc = check_hip(ctx, hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, Tile<B>::LDS),
-                               "raising the dynamic LDS limit"))
-            return rc;
-        attr_set = true;
-    }
-    const int64_t xtiles = ((F == kRowsTimesA ? a.dout : a.din) + B - 1) / B, high = F == kOuterSums ? (a.dout + B - 1) / B : 1, each = high * xtiles;
-    const int64_t items = F == kOuterSums ? most_runs(a.rows, a.K, a.run) : most_tiles(a.rows, a.K, a.offsets, B);
-    const int64_t groups = F != kOuterSums ? ((items * xtiles + 7) / 8 + 2) * 8 : each < 16 ? items * each : (each + 7) / 8 * 8 * items;
-    if (groups * Tile<B>::THREADS >= (int64_t)1 << 32)
-        return fail(ctx, SOM_EINVAL, "%s: more tiles than a launch holds; call with fewer rows or nodes", what);
-    hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(Tile<B>::THREADS), Tile<B>::LDS, ctx->stream, a, (unsigned)xtiles);
-    return check_hip(ctx, hipGetLastError(), what);
-}
-
-// Which tiles a call takes: the estimated time of each size in microseconds, from timed steps of 128 bytes of the contraction.
-//   A workgroup alone on its unit takes 1.1, 0.65 and 0.47 us a step (16-bit; 256, 128 and 64 rows), as many as fit 1.6, 1.35 (two) and 1.3 (five);
-//   float32 goes by its products alone: 7.3, 2.05 and 0.55 us each.  Beside its steps a tile takes some 9, 6 and 4 us.  Small tiles fill the
-//   chip where there are few and waste less of narrow matrices, large ones read less: 65536 rows 2048 -> 1536 on 64 nodes 540, 633 and
-//   954 us, 256 rows 4096 -> 4096 on one 80, 46 and 35, 250,013 rows 37 -> 24 in float32 on 437 nodes 148, 98 and 55.
-template <class T, Form F>
-static double tile_time(const som_ctx* ctx, const ProductArgs<T>& a, int B)
-{
-    const double rows = a.rows, groups = a.K < rows ? a.K : rows, across = ((F == kRowsTimesA ? a.dout : a.din) + B - 1) / B;
-    const double cut = rows / a.run + (a.offsets ? 0.5 * a.K : 0.5), runs = F != kOuterSums ? 1.0 : cut > a.K ? cut : a.K;
-    const double tall = rows / B + (a.offsets ? 0.5 * groups : 0.5);
-    const double tiles = across * (F == kOuterSums ? runs * ((a.dout + B - 1) / B) : tall > groups ? tall : groups);
-    const double depth = F == kRowsTimesA ? a.din : F == kRowsTimesAt ? a.dout : rows / runs;
-    const double steps = 1.0 + depth * sizeof(T) / 128.0, more = B == 256 ? 9.0 : B == 128 ? 6.0 : 4.0, most = B == 256 ? 1.0 : B == 128 ? 2.0 : 5.0;
-    auto step = [&](double o) {                         // o workgroups on a unit
-        if (sizeof(T) == 4) return B == 256 ? 7.3 : B == 128 ? 2.05 * o : 0.55 * o;
-        return B == 256 ? 1.1 + 0.5 * o * o : B == 128 ? 0.65 + 0.7 * (o - 1.0) : 0.47 + 0.05 * (o - 1.0) * (o - 1.0);
-    };
-    const double rounds = tiles / (ctx->units * most), whole = (double)(int64_t)rounds, rest = (rounds - whole) * most;
-    return whole * (steps * step(most) + more) + (rest > 0.0 ? steps * step(B == 256 ? rest : rest < 1.0 ? 1.0 : rest) + more : 0.0);
-}
-
-template <class T, Form F>
-static int product_launch(som_ctx* ctx, const ProductArgs<T>& a, const char* what)
-{
-    const double t256 = tile_time<T, F>(ctx, a, 256), t128 = tile_time<T, F>(ctx, a, 128), t64 = tile_time<T, F>(ctx, a, 64);
-    const bool aligned = product_aligned(a);
-    if (t256 <= t128 && t256 <= t64) return aligned ? product_tile_launch<T, F, 256, true>(ctx, a, what) : product_tile_launch<T, F, 256, false>(ctx, a, what);
-    if (t128 <= t64) return aligned ? product_tile_launch<T, F, 128, true>(ctx, a, what) : product_tile_launch<T, F, 128, false>(ctx, a, what);
-    return aligned ? product_tile_launch<T, F, 64, true>(ctx, a, what) : product_tile_launch<T, F, 64, false>(ctx, a, what);
-}
-
-template <class T>
-int product_typed(som_ctx* ctx, const NodeProduct& p)
-{
-    ProductArgs<T> a{};
-    a.P = (const T*)p.X;
-    a.ldp = p.ldx;
-    a.Q = (const T*)p.A;
-    a.offsets = p.offsets;
-    a.rows = (int)p.rows;
-    a.K = p.K;
-    a.din = p.din;
-    a.dout = p.dout;
-    a.bias = (const T*)p.bias;
-    a.residual = (const T*)p.residual;
-    a.ldr = p.ldr;
-    a.pre = (T*)p.pre;
-    a.ldpre = p.ldpre;
-    a.out = (T*)p.out;
-    a.ldo = p.ldo;
-    a.act = p.act;
-    return product_launch<T, kRowsTimesA>(ctx, a, "product launch");
-}
-
-// Kernel, lanes of a row and columns of a workgroup for the slopes and biases of `dout` columns.
-template <class T>
-static auto slope_kernel_for(int32_t dout, int& lanes, int& columns)
-{
-    constexpr int N = Piece<T>::N;
-    lanes = dout < N ? row_lanes(dout, 8) : row_lanes((dout + N - 1) / N, 64);
-    columns = lanes * (dout < N ? 1 : N);
-    if (dout < N) return lanes == 1 ? slope_kernel<T, 1, 1> : lanes == 2 ? slope_kernel<T, 1, 2> : lanes == 4 ? slope_kernel<T, 1, 4> : slope_kernel<T, 1, 8>;
-    return lanes == 1   ? slope_kernel<T, N, 1>
-           : lanes == 2 ? slope_kernel<T, N, 2>
-           : lanes == 4 ? slope_kernel<T, N, 4>
-           : lanes == 8 ? slope_kernel<T, N, 8>
-           : lanes == 16 ? slope_kernel<T, N, 16>
-           : lanes == 32 ? slope_kernel<T, N, 32>
-                         : slope_kernel<T, N, 64>;
-}
-
-template <class T>
-static int runs_join(som_ctx* ctx, const int32_t* offsets, int32_t K, int64_t rows, int run, const float* parts, int64_t count, T* out)
-{
-    const int64_t longer = rows / ((int64_t)run + 1), y = longer < K ? longer : K;        // groups with more than one run, at most
-    if (y == 0) return SOM_OK;
-    // biases: many runs of few values; matrices: few runs of many
-    if (count <= 16384) {
-        hipLaunchKernelGGL((runs_join_kernel<T, 16>), dim3((unsigned)((count + 63) / 64), (unsigned)y), dim3(1024), 0, ctx->stream, offsets, K, (int)rows,
-                           run, parts, count, out);
-    } else {
-        const int64_t blocks = (count + 255) / 256, share = 16 * ctx->units / y + 1;       // (most of the y find no group)
-        hipLaunchKernelGGL((runs_join_kernel<T, 1>), dim3((unsigned)(blocks < share ? blocks : share), (unsigned)y), dim3(256), 0, ctx->stream, offsets, K,
-                           (int)rows, run, parts, count, out);
-    }
-    return check_hip(ctx, hipGetLastError(), "product gradient join launch");
-}
-
-template <class T>
-int product_grad_typed(som_ctx* ctx, const NodeProductGrad& p)
-{
-    const bool sloped = p.act != SOM_ACT_NONE && p.rows > 0;
-    ProductArgs<T> a{};
-    a.offsets = p.offsets;
-    a.rows = (int)p.rows;
-    a.K = p.K;
-    a.din = p.din;
-    a.dout = p.dout;
-    // workspace: dz, then the runs' sums (of the biases, then of the matrices)
-    int lanes, columns;
-    auto slopes = slope_kernel_for<T>(p.dout, lanes, columns);
-    const int64_t blocks = (p.dout + columns - 1) / columns;
-    const int bias_run = 4096 / lanes;               // four rows at a time and lane, four times
-    a.run = run_rows(ctx, p.rows, p.K, (int64_t)((p.dout + 255) / 256) * ((p.din + 255) / 256), 512);
-    const size_t dz_bytes = sloped ? ((size_t)p.rows * p.dout * sizeof(T) + 255) / 256 * 256 : 0;
-    const size_t bias_parts = p.dbias && p.rows > bias_run ? (size_t)run_slots(p.rows, bias_run) * p.dout : 0;
-    const size_t sum_parts = p.dA && p.rows > a.run ? (size_t)run_slots(p.rows, a.run) * p.dout * p.din : 0;
-    if (dz_bytes + bias_parts + sum_parts)
-        if (int rc = models_workspace(ctx, dz_bytes + (bias_parts > sum_parts ? bias_parts : sum_parts) * sizeof(float))) return rc;
-    T* dz = (T*)ctx->models_blob;
-    float* parts = (float*)((char*)ctx->models_blob + dz_bytes);
-    if (sloped || p.dbias) {
-        const int64_t runs = most_runs(p.rows, p.K, bias_run), y = runs < 32768 ? runs : 32768;
-        hipLaunchKernelGGL(slopes, dim3((unsigned)blocks, (unsigned)y, (unsigned)((runs + y - 1) / y)), dim3(256), 0, ctx->stream, (const T*)p.dY, p.lddy,
-                           (const T*)p.pre, p.ldpre, p.offsets, p.K, (int)p.rows, p.dout, p.act, sloped ? dz : nullptr, (T*)p.dbias, bias_run, parts);
-        if (int rc = check_hip(ctx, hipGetLastError(), "product gradient slope launch")) return rc;
-        if (bias_parts)
-            if (int rc = runs_join(ctx, p.offsets, p.K, p.rows, bias_run, parts, p.dout, (T*)p.dbias)) return rc;
-    }
-    a.P = sloped ? dz : (const T*)p.dY;
-    a.ldp = sloped ? p.dout : p.lddy;
-    if (p.dX && p.rows > 0) {
-        a.Q = (const T*)p.A;
-        a.out = (T*)p.dX;
-        a.ldo = p.lddx;
-        if (int rc = product_launch<T, kRowsTimesAt>(ctx, a, "product gradient (rows) launch")) return rc;
-    }
-    if (p.dA) {
-        a.Q = (const T*)p.X;
-        a.ldq = p.ldx;
-        a.out = (T*)p.dA;
-        a.ldo = p.din;
-        a.parts = parts;
-        if (int rc = product_launch<T, kOuterSums>(ctx, a, "product gradient (matrices) launch")) return rc;
-        if (sum_parts) return runs_join(ctx, p.offsets, p.K, p.rows, a.run, parts, (int64_t)p.dout * p.din, (T*)p.dA);
-    }
-    return SOM_OK;
 }
 
 } // namespace som

@@ -117,7 +117,7 @@ def test_without_memory_for_the_workspace(ctx):
     ctx.limit(16)
     rc, kernels = call(ctx, "som_group", T=100_000)
     assert rc == -2 and kernels == [] and "workspace" in ctx.error()
-    rc, kernels = call(ctx, "som_node_product_grad")
+    rc, kernels = call(ctx, "som_node_product_grad", Din=300, ldx=300, lddx=300)
     assert rc == -2 and kernels == []
     ctx.limit()
     assert call(ctx, "som_group", T=100_000)[0] == SOM_OK
