@@ -1,7 +1,7 @@
 // Launches of the products with the nodes' matrices: which kernels a call takes, runs, workspaces.
 #pragma once
 
-#include "som_product_narrow.hpp"
+#include "som_product_few.hpp"
 
 namespace som {
 
@@ -90,6 +90,7 @@ int product_typed(som_ctx* ctx, const NodeProduct& p)
     a.ldo = p.ldo;
     a.act = p.act;
     if (product_narrow<T>(p.dout, p.din)) return product_narrow_launch<T, false>(ctx, a, "product launch");
+    if (product_few(a)) return product_few_launch(ctx, a, "product launch");
     return product_launch<T, kRowsTimesA>(ctx, a, "product launch");
 }
 
