@@ -47,7 +47,7 @@ static double tile_time(const som_ctx* ctx, const ProductArgs<T>& a, int B)
 {
     const double rows = a.rows, groups = a.K < rows ? a.K : rows, across = ((F == kRowsTimesA ? a.dout : a.din) + B - 1) / B;
     const double cut = rows / a.run + (a.offsets ? 0.5 * a.K : 0.5), runs = F != kOuterSums ? 1.0 : cut > a.K ? cut : a.K;
-    const double tall = rows / B + (a.offsets ? 0.5 * groups : 0.5);
+    const double tall = a.offsets ? rows / B + 0.5 * groups : (a.rows + B - 1) / B;
     const double tiles = across * (F == kOuterSums ? runs * ((a.dout + B - 1) / B) : tall > groups ? tall : groups);
     const double depth = F == kRowsTimesA ? a.din : F == kRowsTimesAt ? a.dout : rows / runs;
     const double steps = 1.0 + depth * sizeof(T) / 128.0, more = B == 256 ? 9.0 : B == 128 ? 6.0 : 4.0, most = B == 256 ? 1.0 : B == 128 ? 2.0 : 5.0;
@@ -57,6 +57,13 @@ static double tile_time(const som_ctx* ctx, const ProductArgs<T>& a, int B)
     };
     const double rounds = tiles / (ctx->units * most), whole = (double)(int64_t)rounds, rest = (rounds - whole) * most;
     return whole * (steps * step(most) + more) + (rest > 0.0 ? steps * step(B == 256 ? rest : rest < 1.0 ? 1.0 : rest) + more : 0.0);
+}
+
+template <class T, Form F>
+static double best_tile_time(const som_ctx* ctx, const ProductArgs<T>& a)
+{
+    const double t256 = tile_time<T, F>(ctx, a, 256), t128 = tile_time<T, F>(ctx, a, 128), t64 = tile_time<T, F>(ctx, a, 64);
+    return t256 < t128 ? (t256 < t64 ? t256 : t64) : t128 < t64 ? t128 : t64;
 }
 
 template <class T, Form F>
@@ -91,6 +98,23 @@ int product_typed(som_ctx* ctx, const NodeProduct& p)
     a.act = p.act;
     if (product_narrow<T>(p.dout, p.din)) return product_narrow_launch<T, false>(ctx, a, "product launch");
     if (product_few(a)) return product_few_launch(ctx, a, "product launch");
+    // The last rows of one node, where they would start another round of tiles: as few rows of their own, in about the time that the matrix
+    // takes to come at 4 TB/s (4099 x 4096 x 4096 f16: 177 us in tiles, .. with three rows apart).
+    const int last = a.rows % 256;
+    if (!a.offsets && a.rows > 256 && last > 0 && last <= 64) {
+        ProductArgs<T> whole = a, rest = a;
+        whole.rows = a.rows - last;
+        rest.rows = last;
+        rest.P = a.P + whole.rows * a.ldp;
+        rest.out = a.out + whole.rows * a.ldo;
+        if (a.residual) rest.residual = a.residual + whole.rows * a.ldr;
+        if (a.pre) rest.pre = a.pre + whole.rows * a.ldpre;
+        const double apart = 6.0 + (double)a.dout * a.din * sizeof(T) / 4e6;
+        if (product_few(rest) && best_tile_time<T, kRowsTimesA>(ctx, whole) + apart < best_tile_time<T, kRowsTimesA>(ctx, a)) {
+            if (int rc = product_launch<T, kRowsTimesA>(ctx, whole, "product launch")) return rc;
+            return product_few_launch(ctx, rest, "product launch");
+        }
+    }
     return product_launch<T, kRowsTimesA>(ctx, a, "product launch");
 }
 
