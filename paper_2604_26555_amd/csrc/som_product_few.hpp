@@ -82,13 +82,14 @@ __global__ void __launch_bounds__(512) product_few_kernel(ProductArgs<T> a, unsi
     }
 }
 
-// Where the matrices' bytes decide: up to 64 rows of one node (4096 -> 4096 bf16: 1 row 31 us by tiles of 64 and 12 like this, 64 rows 34 and 23),
-// and up to 10 of several on average (2048 -> 1536 on 64: 4 each 96 and 91 us, but 32 each 101 and 203, as every sixteen results bring all rows).
+// Where the matrices' bytes decide: up to 64 rows of one node (4096 -> 4096 bf16: 1 row 31 us by tiles of 64 and 11 like this, 64 rows 34 and 23),
+// and up to 10 of several on average, for workgroups that are few or have 64 KB to read (2048 -> 1536 bf16 on 64 nodes: 4 rows each 96 and 90
+// us, but 32 each 101 and 203, as every sixteen results bring all rows; 1024 -> 128 on 700 nodes, 32 KB, 4 rows each: 37 and 55).
 template <class T>
 static bool product_few(const ProductArgs<T>& a)
 {
-    const int64_t groups = a.offsets ? (a.K < a.rows ? a.K : a.rows) : 1;
-    return a.rows <= (a.K > 1 ? 10 : 64) * groups && a.din * (int64_t)sizeof(T) >= 512 && groups * ((a.dout + 15) / 16) < 1 << 22;
+    const int64_t groups = a.offsets ? (a.K < a.rows ? a.K : a.rows) : 1, bytes = a.din * (int64_t)sizeof(T), all = groups * ((a.dout + 15) / 16);
+    return a.rows <= (a.K > 1 ? 10 : 64) * groups && bytes >= 512 && (all <= 2048 || bytes >= 4096) && all < 1 << 22;
 }
 
 template <class T>
