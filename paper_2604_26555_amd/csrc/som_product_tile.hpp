@@ -139,7 +139,8 @@ __device__ __forceinline__ void group_rows(const int32_t* __restrict__ offsets, 
 }
 
 // Where a workgroup finds its work among the groups: a group of n rows has items_of(n) items of two kinds (x and y), and the items are counted in
-// the groups' order.  pick(total) names the item by the totals: (kind, number), kind < 0 for none.  Called by a whole workgroup: the item's
+// the groups' order.  pick(total, kind) names the item by the totals, its number among
+// those of its kind, and leaves kind as it is, below zero, for none.  Called by a whole workgroup: the item's
 // group and which of the group's items it is, or -1.  One pass over the offsets, a stretch of groups a lane, and two barriers.
 struct Item {
     int kind, group, which;
@@ -180,16 +181,17 @@ __device__ __forceinline__ Item find_item(const int32_t* __restrict__ offsets, i
         total.x += sums[w].x;
         total.y += sums[w].y;
     }
-    const int2 picked = pick(total);
-    if (picked.x >= 0) {
-        const unsigned number = (unsigned)picked.y, count = picked.x ? mine.y : mine.x;
-        unsigned at = picked.x ? before.y + incl.y - mine.y : before.x + incl.x - mine.x;
+    int kind = -1;
+    const unsigned number = pick(total, kind);
+    if (kind >= 0) {
+        const unsigned count = kind ? mine.y : mine.x;
+        unsigned at = kind ? before.y + incl.y - mine.y : before.x + incl.x - mine.x;
         if (number >= at && number - at < count) {
             for (int k = k0; k < k1; ++k) {
                 int lo, hi;
                 group_rows(offsets, k, rows, lo, hi);
                 const uint2 n = items_of((unsigned)(hi - lo));
-                const unsigned here = picked.x ? n.y : n.x;
+                const unsigned here = kind ? n.y : n.x;
                 if (number - at < here) {
                     found[0] = k;
                     found[1] = (int)(number - at);
@@ -200,7 +202,7 @@ __device__ __forceinline__ Item find_item(const int32_t* __restrict__ offsets, i
         }
     }
     __syncthreads();
-    return {picked.x, picked.x < 0 ? -1 : __builtin_amdgcn_readfirstlane(found[0]), __builtin_amdgcn_readfirstlane(found[1])};
+    return {kind, kind < 0 ? -1 : __builtin_amdgcn_readfirstlane(found[0]), __builtin_amdgcn_readfirstlane(found[1])};
 }
 
 // The same for items of one kind, by number.
@@ -208,7 +210,11 @@ template <int THREADS, class Items>
 __device__ __forceinline__ int find_group(const int32_t* __restrict__ offsets, int K, int rows, Items items_of, unsigned number, int& which)
 {
     const Item it = find_item<THREADS>(
-        offsets, K, rows, [&](unsigned n) { return make_uint2(items_of(n), 0u); }, [&](uint2) { return make_int2(0, (int)number); });
+        offsets, K, rows, [&](unsigned n) { return make_uint2(items_of(n), 0u); },
+        [&](uint2, int& kind) {
+            kind = 0;
+            return number;
+        });
     which = it.which;
     return it.group;
 }
@@ -464,14 +470,14 @@ __global__ void __launch_bounds__(Tile<B>::THREADS) product_tile_kernel(ProductA
         // uneven nodes, matrices of 6 MB: 530 us with the last tiles last, .. in order).
         const bool apart = a.K == 1;
         const Item it = find_item<THREADS>(
-            a.offsets, a.K, a.rows, [apart](unsigned n) { return apart ? make_uint2(n / BM, n % BM ? 1u : 0u) : make_uint2((n + BM - 1) / BM, 0u); },
-            [&](uint2 total) {
+            a.offsets, a.K, a.rows, [apart](unsigned n) { return make_uint2(apart ? n / BM : (n + BM - 1) / BM, apart && n % BM ? 1u : 0u); },
+            [&](uint2 total, int& kind) __attribute__((always_inline)) {
                 const unsigned whole = total.x * xtiles, run = (whole + 7) / 8, at = xcd * run;
                 const unsigned mine = at < whole ? (whole - at < run ? whole - at : run) : 0u;
-                if (turn < mine) return make_int2(0, (int)banded(at + turn, total.x, xtiles, x));
                 const unsigned rest = total.y * xtiles, last = (rest + 7) / 8, tile = (7 - xcd) * last + turn - mine;
-                if (turn - mine >= last || tile >= rest) return make_int2(-1, 0);
-                return make_int2(1, (int)banded(tile, total.y, xtiles, x));
+                kind = turn < mine ? 0 : turn - mine < last && tile < rest ? 1 : -1;
+                if (kind < 0) return 0u;
+                return banded(kind ? tile : at + turn, kind ? total.y : total.x, xtiles, x);
             });
         if (it.group < 0) return;
         e = it.group;
