@@ -12,6 +12,10 @@ import torch
 F32 = 2.0 ** -24
 SLACK = 1.0 + 2.0 ** -6
 TYPES = [torch.float32, torch.bfloat16, torch.float16]
+# Shapes (M, K, Din, Dout) whose products and gradients take every size of tile, with rows that are aligned and that are not
+TILES = [(2000, 16, 136, 2304), (2001, 16, 137, 2303), (3000, 16, 1536, 136), (3001, 16, 1535, 137), (4500, 16, 136, 2560), (4501, 16, 133, 2559),
+         (6000, 16, 2048, 136), (6001, 16, 2047, 139), (700, 16, 264, 1032), (701, 16, 263, 1033), (700, 16, 1024, 648), (701, 16, 1023, 649),
+         (700, 3, 136, 136), (701, 3, 133, 135), (4100, 1, 512, 4096), (6000, 3, 520, 2304), (6001, 3, 521, 2303), (7000, 6, 1800, 1800)]
 ACTIVATIONS = ["none", "relu", "silu", "gelu", "gelu_tanh"]
 
 
@@ -30,7 +34,7 @@ def rounded(value, error, t):
 
 
 def check(got, want, bound, what):
-    got = got.detach().cpu().double()
+    got, want, bound = got.detach().cpu().double(), want.cpu(), bound.cpu()
     assert got.shape == want.shape, (what, got.shape, want.shape)
     finite = torch.isfinite(want)
     assert torch.equal(torch.isnan(got), torch.isnan(want)), f"{what}: NaN in other places"

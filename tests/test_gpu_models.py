@@ -208,6 +208,76 @@ def test_gradient_of_long_groups(som, M, K, Din, Dout, how, act, dtype):
 
 
 @pytest.mark.parametrize("dtype", ref.TYPES)
+@pytest.mark.parametrize("M, K, Din, Dout", ref.TILES)
+def test_every_size_of_tile(som, M, K, Din, Dout, dtype):
+    """Larger products, against float64 on the GPU: tiles of every size, uneven groups, rows behind the last; twice, to the same bits."""
+    gen = torch.Generator().manual_seed(M + Din)
+    offsets = None if K == 1 else cut(gen, M, K, "tail")
+    with torch.device("cuda"):
+        g = torch.Generator(device="cuda").manual_seed(M)
+        rnd = lambda *s, scale=1.0: (torch.randn(*s, generator=g) * scale).to(dtype)
+        X, A, c, R = rnd(M, Din), rnd(K, Dout, Din, scale=Din ** -0.5), rnd(K, Dout), rnd(M, Dout)
+        dY, Z, before, before_x = rnd(M, Dout), rnd(M, Dout, scale=2.0), rnd(M, Dout), rnd(M, Din)
+        off = None if offsets is None else offsets.cuda()
+        outs = []
+        for _ in range(2):
+            out, pre, dX = before.clone(), before.clone(), before_x.clone()
+            som.som_node_product(X, A, offsets=off, bias=c, activation="gelu", residual=R, pre=pre, out=out)
+            outs.append([out, pre, *som.som_node_product_grad(dY, X, A, offsets=off, pre=Z, activation="silu", dX=dX)])
+        for a, b in zip(*outs):
+            assert torch.equal(a, b)
+        out, pre, dX, dA, dbias = outs[0]
+        y, yb, z, zb = ref.product(X, A, offsets, c, "gelu", R, before, before)
+        ref.check(out, y, yb, "Y")
+        ref.check(pre, z, zb, "pre")
+        grads = ref.product_grad(dY, X, A, offsets, Z, "silu", before_x)
+        for got, i, name in ((dX, 0, "dX"), (dA, 2, "dA"), (dbias, 4, "dbias")):
+            ref.check(got, grads[i], grads[i + 1], name)
+
+
+def test_offsets_behind_four_billion_bytes(som):
+    """Places, rows and matrices further than 2^31 values and 2^32 bytes from their tensors' starts."""
+    M, D = 600_000, 4096                                             # 2.5e9 values, 4.9 GB
+    with torch.device("cuda"):
+        Y = torch.zeros(M, D, dtype=torch.bfloat16)
+        X = torch.randn(3, D).bfloat16()
+        slot = torch.tensor([[M - 1], [7], [550_001]], dtype=torch.int32)
+        som.som_dispatch(X, slot, out=Y)
+        som.som_sync()
+        assert torch.equal(Y[slot[:, 0].long()], X) and int((Y[524_288:] != 0).any(1).sum()) == 2
+        assert torch.equal(som.som_combine(Y, slot), X)
+        A = (torch.randn(2, 8, D) / 64).bfloat16()
+        offsets = torch.tensor([M - 70, M - 5, M], dtype=torch.int32)         # the last seventy rows
+        out = torch.zeros(M, 8, dtype=torch.bfloat16)
+        som.som_node_product(Y, A, offsets=offsets, out=out)
+        x, a = Y[M - 1].double(), A[1].double()
+        assert ((out[M - 1].double() - a @ x).abs() <= 2.0 ** -8 * (a @ x).abs() + D * ref.F32 * (a.abs() @ x.abs())).all() and not out[:M - 70].any()
+        dY = torch.zeros(M, 8, dtype=torch.bfloat16)
+        dY[M - 1] = 1.0
+        _, dA, dbias = som.som_node_product_grad(dY, Y, A, offsets=offsets, dX=False)
+        assert torch.equal(dA[1], Y[M - 1].expand(8, D)) and not dA[0].any() and torch.equal(dbias, torch.tensor([[0.0], [1.0]]).expand(2, 8).bfloat16())
+        dX = som.som_node_product_grad(dY, Y, A, offsets=offsets, dX=torch.zeros_like(Y), dA=False, dbias=False)[0]
+        want = a.sum(0)
+        assert ((dX[M - 1].double() - want).abs() <= 2.0 ** -8 * want.abs() + 8 * ref.F32 * a.abs().sum(0)).all() and int((dX != 0).any(1).sum()) == 1
+    del Y, dX, out, dY
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("Din, Dout, M", [(64, 40, 300), (2048, 64, 9), (256, 256, 300)])
+def test_small_half_precision_values_count(som, Din, Dout, M):
+    """float16 rows below its normal range (6e-5) are not taken for zeros."""
+    gen = torch.Generator().manual_seed(9)
+    X, A = normal(gen, M, Din, dtype=torch.float16, scale=2.0 ** -18), normal(gen, Dout, Din, dtype=torch.float16)
+    zero = torch.zeros(M, Dout, dtype=torch.float16)
+    Y = som.som_node_product(X.cuda(), A.cuda())
+    want, bound, _, _ = ref.product(X, A, None, None, "none", None, zero, zero)
+    ref.check(Y, want, bound, "Y")
+    assert float(want.abs().mean()) > 4 * float(bound.mean())
+    dX, dA, _ = som.som_node_product_grad(normal(gen, M, Dout, dtype=torch.float16).cuda(), X.cuda(), A.cuda())
+    assert float(dA.float().abs().mean()) > 0
+
+
+@pytest.mark.parametrize("dtype", ref.TYPES)
 def test_product_without_rows(som, dtype):
     X, A = torch.empty(0, 24, dtype=dtype, device="cuda"), torch.randn(3, 8, 24, device="cuda").to(dtype)
     offsets = torch.zeros(4, dtype=torch.int32, device="cuda")

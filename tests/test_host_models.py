@@ -131,6 +131,63 @@ def test_group_routes(ctx, T, k, K, launches):
     assert rc == SOM_OK and len(kernels) == launches, kernels
 
 
+def tiles_of(ctx, name, **changes):
+    """Rows of the tiles that a call launches (a workgroup's LDS is 512 bytes a row), in order."""
+    call(ctx, name, **changes)
+    return [lds // 512 for kernel, _, _, _, _, lds in ctx.launches if "product_tile" in kernel]
+
+
+def test_shapes_take_every_tile(ctx):
+    """The shapes of the GPU tests reach tiles of 64, 128 and 256 rows in the product and in both gradients, aligned and not."""
+    seen = set()
+    for M, K, Din, Dout in ref.TILES:
+        off = "p" if K > 1 else None
+        for t, E in ((0, 4), (1, 8), (2, 8)):
+            aligned = Din % E == 0 and Dout % E == 0
+            for b in tiles_of(ctx, "som_node_product", type=t, M=M, K=K, offsets=off, Din=Din, ldx=Din, Dout=Dout, ldr=Dout, ldpre=Dout, ldy=Dout):
+                seen.add((t > 0, "product", b, aligned))
+            grad = dict(type=t, M=M, K=K, offsets=off, Din=Din, ldx=Din, lddx=Din, Dout=Dout, lddy=Dout, ldpre=Dout, act=0, pre=None, dbias=None)
+            for b in tiles_of(ctx, "som_node_product_grad", dA=None, **grad):
+                seen.add((t > 0, "dX", b, aligned))
+            for b in tiles_of(ctx, "som_node_product_grad", dX=None, **grad):
+                seen.add((t > 0, "dA", b, aligned))
+    want = {(half, form, b, aligned) for half in (True, False) for form in ("product", "dX", "dA") for b in (64, 128, 256) for aligned in (True, False)}
+    assert want - seen == set()
+
+
+ROUTES = [  # call, changes, kernels in order
+    # narrow rows: up to 64 results and 256 bytes of the contraction
+    ("som_node_product", dict(M=5000, Din=64, ldx=64, Dout=64, ldr=64, ldpre=64, ldy=64), ["product_narrow"]),
+    ("som_node_product", dict(M=5000, Din=65, ldx=65, Dout=64, ldr=64, ldpre=64, ldy=64), ["product_tile"]),
+    ("som_node_product", dict(M=5000, Din=64, ldx=64, Dout=65, ldr=65, ldpre=65, ldy=65), ["product_tile"]),
+    ("som_node_product", dict(type=1, M=5000, Din=128, ldx=128, Dout=64, ldr=64, ldpre=64, ldy=64), ["product_narrow"]),
+    ("som_node_product", dict(type=1, M=5000, Din=129, ldx=129, Dout=64, ldr=64, ldpre=64, ldy=64), ["product_tile"]),
+    # few rows: ten a node, or 64 of one
+    ("som_node_product", dict(type=1, M=50, Din=2048, ldx=2048, Dout=256, ldr=256, ldpre=256, ldy=256), ["product_few"]),
+    ("som_node_product", dict(type=1, M=51, Din=2048, ldx=2048, Dout=256, ldr=256, ldpre=256, ldy=256), ["product_tile"]),
+    ("som_node_product", dict(type=1, M=64, K=1, offsets=None, Din=512, ldx=512, Dout=256, ldr=256, ldpre=256, ldy=256), ["product_few"]),
+    ("som_node_product", dict(type=1, M=65, K=1, offsets=None, Din=512, ldx=512, Dout=256, ldr=256, ldpre=256, ldy=256), ["product_tile"]),
+    ("som_node_product", dict(type=1, M=64, K=1, offsets=None, Din=255, ldx=255, Dout=256, ldr=256, ldpre=256, ldy=256), ["product_tile"]),
+    # one node's last rows apart where they would start another round, and in the tiles where they would not
+    ("som_node_product", dict(type=2, M=4099, K=1, offsets=None, Din=4096, ldx=4096, Dout=4096, ldr=4096, ldpre=4096, ldy=4096), ["product_tile", "product_few"]),
+    ("som_node_product", dict(type=2, M=4000, K=1, offsets=None, Din=4096, ldx=4096, Dout=4096, ldr=4096, ldpre=4096, ldy=4096), ["product_tile"]),
+    # gradients: slopes and biases in a pass of their own, joins where a group can have more than one run; float32 narrow sums in one
+    ("som_node_product_grad", dict(type=1, M=300, Din=300, ldx=300, lddx=300), ["slope", "product_tile", "product_tile"]),
+    ("som_node_product_grad", dict(type=1, M=9000, Din=300, ldx=300, lddx=300), ["slope", "product_tile", "product_tile", "runs_join", "runs_join"]),
+    ("som_node_product_grad", dict(type=1, M=300, Din=300, ldx=300, lddx=300, act=0, dbias=None), ["product_tile", "product_tile"]),
+    ("som_node_product_grad", dict(type=1, M=300, Din=16, dA=None, dbias=None), ["product_narrow"]),
+    ("som_node_product_grad", dict(type=0, M=200, Din=64, ldx=64, lddx=64), ["product_narrow", "sums_narrow"]),
+    ("som_node_product_grad", dict(type=0, M=9000, Din=64, ldx=64, lddx=64), ["product_narrow", "sums_narrow", "runs_join", "runs_join"]),
+    ("som_node_product_grad", dict(type=0, M=200, Din=64, ldx=64, lddx=64, dX=None, dA=None), ["sums_narrow"]),
+]
+
+
+@pytest.mark.parametrize("name, changes, kernels", ROUTES)
+def test_routes(ctx, name, changes, kernels):
+    rc, got = call(ctx, name, **changes)
+    assert rc == SOM_OK and len(got) == len(kernels) and all(k in g for k, g in zip(kernels, got)), got
+
+
 def test_a_failed_launch_is_reported(ctx):
     for name in CALLS:
         rc, kernels = call(ctx, name)
