@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(256) group_hist_kernel(const int32_t* __restri
     const int64_t block = run_of_die(groups) * (blockDim.x >> 6) + wave;
     uint32_t* count = group_lds + wave * (K + 1);
     for (int k = lane; k <= K; k += 64) count[k] = 0u;
-    __builtin_amdgcn_wave_barrier();
+    wave_in_order();
     if (block >= blocks) return;                              // (no barrier: a wavefront works on its own)
     const int64_t lo = block * per_block, hi = lo + per_block < pairs ? lo + per_block : pairs;
     for (int64_t p = lo + lane; p < hi; p += 256) {
@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(256) group_hist_kernel(const int32_t* __restri
         for (int u = 0; u < 4; ++u)
             if (b[u] >= 0) atomicAdd(&count[b[u]], 1u);
     }
-    __builtin_amdgcn_wave_barrier();
+    wave_in_order();
     for (int k = lane; k <= K; k += 64) hist[(size_t)block * (K + 1) + k] = count[k];
 }
 
@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(256) group_scatter_kernel(const int32_t* __res
     if (block >= blocks) return;                              // (no barrier below: a wavefront works on its own)
     uint32_t* place = group_lds + wave * (K + 1);
     for (int k = lane; k <= K; k += 64) place[k] = (OWN ? starts[k] : start[k]) + hist[(size_t)block * (K + 1) + k];
-    __builtin_amdgcn_wave_barrier();
+    wave_in_order();
     const int64_t lo = block * per_block, hi = lo + per_block < pairs ? lo + per_block : pairs;
     scatter_pairs(node, lo, hi, K, place, order, slot);
 }

@@ -1,6 +1,6 @@
 // Products of narrow rows: up to 64 results and 256 bytes of the contraction (64 floats, 128 16-bit values), as the local models of a table
-// have them.  What bounds them is memory; a node's matrix stays in a wavefront's registers, rows come as the matrix pipe takes them straight from
-// memory, and there is neither LDS nor a barrier on the way.
+// have them.  What bounds them is memory; a node's matrix stays in a wavefront's registers, rows pass through LDS that is the wavefront's own, and
+// there is no barrier on the way.
 #pragma once
 
 #include "som_product_tile.hpp"
@@ -129,6 +129,7 @@ __global__ void __launch_bounds__(256) product_narrow_kernel(ProductArgs<T> a, i
             for (int j = 0; j < E; ++j) x[j] = j < again[i] ? (T)0.0f : x[j];
             if (row_of[i] < 32) *reinterpret_cast<Frag*>(mine + (row_of[i] * kRow + (from[i] + again[i]) / E) * 16) = x;
         }
+        wave_in_order();
         fetch(b + 4);
         f32x16 acc[V] = {};
 #pragma unroll
@@ -140,12 +141,14 @@ __global__ void __launch_bounds__(256) product_narrow_kernel(ProductArgs<T> a, i
         }
         // a lane has its row's results, four consecutive ones at a time; they go out in the order of memory
         float* turned = reinterpret_cast<float*>(mine);
+        wave_in_order();
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
             for (int g = 0; g < 4; ++g)
                 *reinterpret_cast<float4*>(turned + (lane & 31) * kOut + 32 * v + 8 * g + 4 * h) =
                     make_float4(acc[v][4 * g], acc[v][4 * g + 1], acc[v][4 * g + 2], acc[v][4 * g + 3]);
+        wave_in_order();
         constexpr int G = E;                              // results of a lane at a time
         const int groups = (Nn + G - 1) / G;
 #pragma unroll 1
@@ -193,6 +196,7 @@ __global__ void __launch_bounds__(256) product_narrow_kernel(ProductArgs<T> a, i
             for (int j = 0; j < G; ++j) y.e[j] = (T)x[j];
             store(y, a.out + row * a.ldo + n);
         }
+        wave_in_order();
     }
 }
 

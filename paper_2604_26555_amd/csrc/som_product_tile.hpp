@@ -467,7 +467,7 @@ __global__ void __launch_bounds__(Tile<B>::THREADS) product_tile_kernel(ProductA
     } else {
         // One node: whole tiles (kind 0) first, its last ones (kind 1), which take less time, when those run out (4099 x 4096 x 4096: 213 us in
         // order, 178 like this).  Several: all of a group's tiles together, so that its matrix comes once (65536 rows 2048 -> 1536 on 64
-        // uneven nodes, matrices of 6 MB: 530 us with the last tiles last, .. in order).
+        // uneven nodes, matrices of 6 MB: 530 us with the last tiles last, 509 in order).
         const bool apart = a.K == 1;
         const Item it = find_item<THREADS>(
             a.offsets, a.K, a.rows, [apart](unsigned n) { return make_uint2(apart ? n / BM : (n + BM - 1) / BM, apart && n % BM ? 1u : 0u); },
@@ -645,6 +645,7 @@ __global__ void __launch_bounds__(Tile<B>::THREADS) product_tile_kernel(ProductA
                     *reinterpret_cast<float4*>(turned + (lane & 31) * kRow + 32 * v + 8 * g + 4 * (lane >> 5)) = x;
                 }
         }
+        wave_in_order();
 #pragma unroll 1
         for (int r = lane / kLanes; r < 32; r += kAtOnce) {
             const int64_t row = row0 + r;
@@ -679,6 +680,7 @@ __global__ void __launch_bounds__(Tile<B>::THREADS) product_tile_kernel(ProductA
             T* out = F == kOuterSums ? a.out + ((int64_t)e * a.dout + row) * a.din : a.out + row * a.ldo;
             store8(y, out + n);
         }
+        wave_in_order();
     }
 }
 

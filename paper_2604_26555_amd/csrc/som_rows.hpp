@@ -24,6 +24,13 @@ __device__ __forceinline__ int64_t piece_at(int c, int D)
     return at + N <= D ? at : D - N;
 }
 
+// A wavefront's writes to LDS before, its reads behind (the same wavefront's LDS accesses take effect in order).
+__device__ __forceinline__ void wave_in_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // Lanes that share a row of `pieces` pieces: a power of two, at most `most`.
 inline int row_lanes(int64_t pieces, int most)
 {
