@@ -322,8 +322,9 @@ int som_epoch_file(som_ctx* ctx, int fd, int64_t offset, int64_t N, int32_t D, i
  * T rows with k nodes each are the pairs p = t k + j.  Pairs whose node lies outside [0, K) (padding, a row that found no place)
  * have no place, contribute nothing and get nothing.  M is the number of places a sorted matrix holds (T k, or more); places from
  * offsets[K] on belong to no node, and what calls would write there is left as it was.  Entries of slot and offsets that point outside
- * M are not followed.  Matrices have leading dimensions of their own (>= their width, <= 2^21), any alignment of their elements serves;
- * widths are at most 2^20, T k and M at most 2^31 - 1, K at most 32768.  Outputs must not overlap inputs or one another.
+ * M are not followed.  No two pairs share a place (where they do, the place's row is a mixture of what either writes).  Matrices have
+ * leading dimensions of their own (>= their width, <= 2^21), any alignment of their elements serves; widths are at most 2^20, T k and M
+ * at most 2^31 - 1 (products: M at most 2^31 - 65536), K at most 32768.  Outputs must not overlap inputs or one another.
  */
 enum { SOM_ROWS_FLOAT = 0 /* float32 */, SOM_ROWS_BFLOAT = 1 /* bfloat16 */, SOM_ROWS_HALF = 2 /* float16 */ };
 

@@ -433,6 +433,7 @@ static int models_checks(som_ctx* ctx, int type, int64_t M, int32_t Din, int32_t
 {
     if (int rc = rows_checks(ctx, type, M, Din, "X")) return rc;
     if (int rc = rows_checks(ctx, type, M, Dout, "Y")) return rc;
+    if (M > kModelRows) return fail(ctx, SOM_EINVAL, "X: more than 2^31-65536 rows per call");
     if (K < 1 || K > kGroupNodes) return fail(ctx, SOM_EINVAL, "K (%d) outside 1..%d", K, kGroupNodes);
     if (!offsets && K != 1) return fail(ctx, SOM_EINVAL, "without offsets there is one node (K=%d)", K);
     if (activation < SOM_ACT_NONE || activation > SOM_ACT_GELU_TANH) return fail(ctx, SOM_EINVAL, "unknown activation %d", activation);

@@ -394,7 +394,7 @@ class Som:
         rows, columns, ld = _matrix(t, name)
         if shape is not None and (rows, columns) != shape:
             raise ValueError(f"{name} must be {shape[0]} x {shape[1]}, got {rows} x {columns}")
-        return t.data_ptr(), rows, columns, ld
+        return t.data_ptr(), rows, columns, ld if rows > 1 else columns
 
     def _pairs(self, t, name, dtype):
         """(address, rows, nodes per row) of an array with an entry for each pair of row and node: (T,) or (T, k)."""

@@ -451,6 +451,20 @@ def test_outputs_made_for_a_stream_of_their_own(som):
     mine.close()
 
 
+@pytest.mark.parametrize("D", [2, 40, 300])
+def test_the_same_place_twice(som, D):
+    """Pairs of one row that share a place: read twice by the sum, written twice with the same values; a single row of any stride."""
+    X = torch.randn(50, D, device="cuda")
+    slot = torch.arange(50, dtype=torch.int32, device="cuda")[:, None].repeat(1, 3)
+    assert torch.equal(som.som_dispatch(X, slot, out=torch.empty_like(X)), X)
+    assert torch.equal(som.som_combine(X, slot), X + X + X)
+    dY, dw = som.som_combine_grad(X, X, slot)
+    assert torch.equal(dY, X) and torch.equal(dw[:, 0], dw[:, 2])
+    row = torch.as_strided(torch.randn(D, device="cuda"), (1, D), (2 ** 22, 1))
+    assert torch.equal(som.som_dispatch(row, slot[:1, :1]), row)
+    assert torch.equal(som.som_node_product(row, torch.eye(D, device="cuda")), row)
+
+
 def test_python_refusals(som):
     X, A = torch.zeros(6, 8, device="cuda"), torch.zeros(2, 4, 8, device="cuda")
     off, slot = torch.tensor([0, 3, 6], dtype=torch.int32, device="cuda"), torch.zeros(6, 1, dtype=torch.int32, device="cuda")

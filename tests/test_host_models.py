@@ -74,6 +74,7 @@ REFUSED = [
     ("som_node_product", dict(ldpre=7), "pre: leading"), ("som_node_product", dict(ldy=7), "Y: leading"),
     ("som_node_product_grad", dict(dX=None, dA=None, dbias=None), "none of"), ("som_node_product_grad", dict(pre=None), "pre"),
     ("som_node_product_grad", dict(dY=None), "dY"), ("som_node_product_grad", dict(X=None), "X"), ("som_node_product_grad", dict(A=None), "A"),
+    ("som_node_product", dict(M=2 ** 31 - 65535), "2^31-65536"), ("som_node_product_grad", dict(M=2 ** 31 - 1), "2^31-65536"),
     ("som_node_product_grad", dict(lddx=15), "dX: leading"), ("som_node_product_grad", dict(offsets=None), "one node"),
 ]
 
