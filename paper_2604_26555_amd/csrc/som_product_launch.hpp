@@ -165,15 +165,15 @@ int product_grad_typed(som_ctx* ctx, const NodeProductGrad& p)
     a.K = p.K;
     a.din = p.din;
     a.dout = p.dout;
-    // What applies the slopes: narrow kernels as they read dY, of float32 all of them; else a pass that stores dz (and sums the biases).
+    // What applies the slopes: narrow kernels as they read dY; else a pass that stores dz (and sums the biases).
     const bool sloped = p.act != SOM_ACT_NONE && p.rows > 0, narrow_rows = product_narrow<T>(p.din, p.dout);
-    const bool narrow_sums = sizeof(T) == 4 && narrow_rows && p.dout <= kNarrow;
-    const bool stored = sloped && !narrow_sums && (p.dA || p.dbias || !narrow_rows);
+    const bool narrow_both = narrow_rows && p.dout <= kNarrow;
+    const bool stored = sloped && !narrow_both && (p.dA || p.dbias || !narrow_rows);
     int lanes, columns;
     auto slopes = slope_kernel_for<T>(p.dout, lanes, columns);
     const int64_t blocks = (p.dout + columns - 1) / columns;
-    a.run = narrow_sums ? narrow_run(ctx, p.rows, p.K) : run_rows(ctx, p.rows, p.K, (int64_t)((p.dout + 255) / 256) * ((p.din + 255) / 256), 512);
-    const int bias_run = narrow_sums ? a.run : 4096 / lanes;               // (else four rows at a time and lane, four times)
+    a.run = narrow_both ? narrow_run(ctx, p.rows) : run_rows(ctx, p.rows, p.K, (int64_t)((p.dout + 255) / 256) * ((p.din + 255) / 256), 512);
+    const int bias_run = narrow_both ? a.run : 4096 / lanes;               // (else four rows at a time and lane, four times)
     // workspace: dz, the runs' sums of the matrices, those of the biases
     auto pieces = [](size_t bytes) { return (bytes + 255) / 256 * 256; };
     const size_t dz_bytes = stored ? pieces((size_t)p.rows * p.dout * sizeof(T)) : 0;
@@ -184,7 +184,12 @@ int product_grad_typed(som_ctx* ctx, const NodeProductGrad& p)
     T* dz = (T*)ctx->models_blob;
     a.parts = (float*)((char*)ctx->models_blob + dz_bytes);
     float* bias_parts = (float*)((char*)a.parts + sum_bytes);
-    if (!narrow_sums && (stored || p.dbias)) {
+    if (narrow_both && (p.dA || p.dbias || p.rows > 0)) {
+        GradientArgs<T> g{(const T*)p.dY, p.lddy, (const T*)p.X, p.ldx, (const T*)p.A, (const T*)p.pre, p.ldpre, p.offsets, (int)p.rows, p.K, p.din, p.dout,
+                          p.act, a.run, (T*)p.dX, p.lddx, (T*)p.dA, (T*)p.dbias, a.parts, bias_parts};
+        if (int rc = gradient_narrow_launch(ctx, g)) return rc;
+    }
+    if (!narrow_both && (stored || p.dbias)) {
         const int64_t runs = most_runs(p.rows, p.K, bias_run), y = runs < 32768 ? runs : 32768;
         hipLaunchKernelGGL(slopes, dim3((unsigned)blocks, (unsigned)y, (unsigned)((runs + y - 1) / y)), dim3(256), 0, ctx->stream, (const T*)p.dY, p.lddy,
                            (const T*)p.pre, p.ldpre, p.offsets, p.K, (int)p.rows, p.dout, p.act, stored ? dz : nullptr, (T*)p.dbias, bias_run, bias_parts);
@@ -195,7 +200,7 @@ int product_grad_typed(som_ctx* ctx, const NodeProductGrad& p)
     a.act = stored ? SOM_ACT_NONE : p.act;
     a.pre = (T*)p.pre;
     a.ldpre = p.ldpre;
-    if (p.dX && p.rows > 0) {
+    if (!narrow_both && p.dX && p.rows > 0) {
         a.Q = (const T*)p.A;
         a.out = (T*)p.dX;
         a.ldo = p.lddx;
@@ -207,15 +212,7 @@ int product_grad_typed(som_ctx* ctx, const NodeProductGrad& p)
     a.ldq = p.ldx;
     a.out = (T*)p.dA;
     a.ldo = p.din;
-    if constexpr (sizeof(T) == 4) {
-        if (narrow_sums && (p.dA || p.dbias)) {
-            auto kern = p.dout <= 32 ? (p.din <= 32 ? sums_narrow_kernel<1, 1> : sums_narrow_kernel<1, 2>)
-                                     : (p.din <= 32 ? sums_narrow_kernel<2, 1> : sums_narrow_kernel<2, 2>);
-            hipLaunchKernelGGL(kern, dim3((unsigned)most_runs(p.rows, p.K, a.run)), dim3(256), 0, ctx->stream, a, (float*)p.dbias, bias_parts);
-            if (int rc = check_hip(ctx, hipGetLastError(), "product gradient (matrices) launch")) return rc;
-        }
-    }
-    if (!narrow_sums && p.dA)
+    if (!narrow_both && p.dA)
         if (int rc = product_launch<T, kOuterSums>(ctx, a, "product gradient (matrices) launch")) return rc;
     if (bias_bytes)
         if (int rc = runs_join(ctx, p.offsets, p.K, p.rows, bias_run, bias_parts, p.dout, (T*)p.dbias)) return rc;

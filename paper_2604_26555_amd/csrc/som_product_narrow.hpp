@@ -200,13 +200,111 @@ __global__ void __launch_bounds__(256) product_narrow_kernel(ProductArgs<T> a, i
     }
 }
 
-// Sums over a run of a group's rows of float32: dA (out not null) and dbias (likewise) at once, slopes applied on the way.  Four wavefronts take
-// every fourth block of eight rows; U and V: blocks of 32 results and features.
-template <int U, int V>
-__global__ void __launch_bounds__(256) sums_narrow_kernel(ProductArgs<float> a, float* __restrict__ dbias, float* __restrict__ bias_parts)
+// Step j of a contraction over 32 rows in LDS, `stride` bytes apart, as the matrix pipe takes them: columns c0 .. + 31, eight rows (floats) or
+// sixteen at a time.
+template <class T>
+__device__ __forceinline__ typename Fragment<T>::type columns(const char* rows, int stride, int c0, int j, int lane)
 {
-    constexpr int kAhead = 4;             // blocks of rows that are on their way together
-    __shared__ float sums[4][V * 16][64];
+    union {
+        typename Fragment<T>::type v;
+        s16x4 s[2];
+    } f;
+    if constexpr (sizeof(T) == 4) {
+        const char* p = rows + (8 * j + 4 * (lane >> 5)) * stride + (c0 + (lane & 31)) * 4;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) f.v[s] = *reinterpret_cast<const float*>(p + s * stride);
+    } else {
+        typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+        const int row = 16 * j + 8 * (lane >> 5) + ((lane & 15) >> 2), col = c0 + (lane & 16) + 4 * (lane & 3);
+        const char* p = rows + row * stride + col * 2;
+        f.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(s16x4*)p);
+        f.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(s16x4*)(p + 4 * stride));
+    }
+    return f.v;
+}
+
+// Chunks of 32 rows of `values` values in the order of memory, chunk number lane + 64 i: what a lane brings.
+template <class T, int S>
+struct Block {
+    static constexpr int E = 16 / sizeof(T), kRow = 2 * S + 1;       // LDS rows in chunks, an odd number of them
+    typedef typename Fragment<T>::type Frag;
+    typedef Frag Any __attribute__((aligned(sizeof(T))));
+    int values, row[S], from[S];
+    bool again[S];                                   // a row's last chunk where it is not whole: the row's last sixteen bytes
+    __device__ __forceinline__ void init(int n, int lane)
+    {
+        values = n;
+        const int chunks = (n + E - 1) / E;
+#pragma unroll
+        for (int i = 0; i < S; ++i) {
+            const int c = lane + 64 * i;
+            row[i] = c / chunks;
+            const int at = (c - row[i] * chunks) * E;
+            again[i] = n >= E && at + E > n;
+            from[i] = again[i] ? n - E : at;
+        }
+    }
+    // those of the rows before `left`, zeros for the others
+    __device__ __forceinline__ Frag load(int i, const T* base, int64_t ld, int left) const
+    {
+        Frag x = {};
+        if (row[i] >= 32 || row[i] >= left) return x;
+        const T* p = base + row[i] * (int)ld + from[i];             // (32 rows of at most 2^21 values)
+        if (values >= E) return *reinterpret_cast<const Any*>(p);
+#pragma unroll
+        for (int j = 0; j < E; ++j)
+            if (j < values) x[j] = p[j];
+        return x;
+    }
+    __device__ __forceinline__ void store(int i, char* lds, Frag x) const
+    {
+        if (row[i] >= 32) return;
+        char* to = lds + row[i] * kRow * 16 + from[i] * (int)sizeof(T);
+        if (again[i]) *reinterpret_cast<Any*>(to) = x;
+        else *reinterpret_cast<Frag*>(to) = x;
+    }
+};
+
+template <class T>
+struct GradientArgs {
+    const T* dY;
+    int64_t lddy;
+    const T* X;                // null where dA is
+    int64_t ldx;
+    const T* A;
+    const T* pre;
+    int64_t ldpre;
+    const int32_t* offsets;
+    int rows;
+    int32_t K, din, dout;
+    int act, run;
+    T* dX;                     // each of them or null
+    int64_t lddx;
+    T *dA, *dbias;
+    float *parts, *bias_parts; // sums of groups with more than one run
+};
+
+// The whole gradient where rows are narrow both ways (64 values each at most): dY, pre and X are read once.  A workgroup takes a run of a group's rows,
+// each of its four wavefronts every fourth block of 32, which pass through LDS of its own: dz by rows for dX, dz and X by columns for dA, whose
+// sums stay in registers until the wavefronts add theirs up in order.  U and V: blocks of 32 results and features.  The matrix lies in LDS as
+// well: in registers it leaves one wavefront a SIMD instead of two (250,013 rows 37 -> 24 in float32 on 437 nodes 109 us, 81 like this).
+// Slopes, rows and sums in passes of their own took 86 us there (floor of the bytes 26), 71 for 200,000 rows 64 -> 64 bf16 on 16 nodes (now
+// 44, floor 22), 88 for 250,000 rows 37 -> 24 bf16 on 437 (now 49, floor 13).  What is left is the matrix pipe's float32 rate on blocks of
+// 32 that are half empty, and a run's start and end.
+template <class T, int U, int V>
+struct Gradient {
+    static constexpr int S = U * sizeof(T), SX = V * sizeof(T), kOut = 32 * V + 4;
+    static constexpr int kRows = 32 * Block<T, S>::kRow * 16, kRowsX = 32 * Block<T, SX>::kRow * 16, kTurned = 32 * kOut * 4;
+    static constexpr int kWave = kRows + (kRowsX > kTurned ? kRowsX : kTurned), kMatrix = V * S * 1024, LDS = 4 * kWave + kMatrix;
+};
+template <class T, int U, int V>
+__global__ void __launch_bounds__(256) gradient_narrow_kernel(GradientArgs<T> a)
+{
+    typedef Gradient<T, U, V> G;
+    typedef typename Fragment<T>::type Frag;
+    constexpr int E = 16 / sizeof(T), S = G::S, SX = G::SX, kOut = G::kOut, kSteps = sizeof(T);     // (32 rows, eight floats or sixteen 16-bit values a step)
+    static_assert(G::LDS >= 4 * V * 4096);
+    extern __shared__ __align__(16) char narrow_lds[];
     __shared__ float bias_sums[4][U * 32];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, l = lane & 31;
     int which, first, end;
@@ -217,72 +315,140 @@ __global__ void __launch_bounds__(256) sums_narrow_kernel(ProductArgs<float> a, 
     const int lo = first, group = end - first;
     first += which * run;
     end = end - first > run ? first + run : end;
+    char *rows = narrow_lds + wave * G::kWave, *rows_x = rows + G::kRows;
+    float* turned = reinterpret_cast<float*>(rows_x);
+    Block<T, S> P;
+    Block<T, SX> Q;
+    P.init(a.dout, lane);
+    Q.init(a.din, lane);
+    Frag next[S], zs[S], xs[SX];
+    auto fetch = [&](int b) __attribute__((always_inline)) {
+        const int64_t row0 = first + 32 * (int64_t)b;
+        const int left = end - first - 32 * b;
+#pragma unroll
+        for (int i = 0; i < S; ++i) {
+            next[i] = P.load(i, a.dY + row0 * a.lddy, a.lddy, left);
+            zs[i] = Frag{};
+            if (a.act) zs[i] = P.load(i, a.pre + row0 * a.ldpre, a.ldpre, left);
+        }
+        if (a.dA)
+#pragma unroll
+            for (int i = 0; i < SX; ++i) xs[i] = Q.load(i, a.X + row0 * a.ldx, a.ldx, left);
+    };
+    fetch(wave);                                      // (on their way while the matrix comes)
+    char* matrix = narrow_lds + 4 * G::kWave;         // as the matrix pipe takes it, block v and step s: 64 chunks
+    if (a.dX) {
+        for (int i = wave; i < V * S; i += 4) {
+            const int n = i / S * 32 + l, k0 = (2 * (i % S) + h) * E;
+            Frag x = {};
+#pragma unroll
+            for (int j = 0; j < E; ++j)
+                if (n < a.din && k0 + j < a.dout) x[j] = a.A[((int64_t)e * a.dout + k0 + j) * a.din + n];
+            *reinterpret_cast<Frag*>(matrix + (i * 64 + lane) * 16) = x;
+        }
+    }
+    // what lies behind dz's columns meets zeros of the matrix, and has to be a number
+    for (int i = lane; i < G::kRows / 16; i += 64) reinterpret_cast<v4i*>(rows)[i] = v4i{};
+    __syncthreads();
     f32x16 acc[U][V] = {};
     float bias[U] = {};
-    int in_p[4], in_z[4], in_q[4];                    // a lane's rows of a block of eight (at most 2^21 values each)
+    for (int b = wave; first + 32 * b < end; b += 4) {
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-        in_p[s] = (4 * h + s) * (int)a.ldp + l;
-        in_z[s] = (4 * h + s) * (int)a.ldpre + l;
-        in_q[s] = (4 * h + s) * (int)a.ldq + l;
-    }
-    for (int b0 = wave; first + 8 * b0 < end; b0 += 4 * kAhead) {
-        f32x4 p[kAhead][U], z[kAhead][U], q[kAhead][V];
+        for (int i = 0; i < S; ++i) {
+            Frag x = next[i];
+            if (a.act) {
+                Piece<T> g = __builtin_bit_cast(Piece<T>, x);
+                slopes<T, E>(g, __builtin_bit_cast(Piece<T>, zs[i]), a.act);
+                x = __builtin_bit_cast(Frag, g);
+            }
+            P.store(i, rows, x);
+        }
+        if (a.dA)
 #pragma unroll
-        for (int w = 0; w < kAhead; ++w) {
-            const int64_t row0 = first + 8 * (int64_t)(b0 + 4 * w);
-            const int left = end - first - 8 * (b0 + 4 * w);
-            const float *P = a.P + row0 * a.ldp, *Z = a.pre + row0 * a.ldpre, *Q = a.Q + row0 * a.ldq;
+            for (int i = 0; i < SX; ++i) Q.store(i, rows_x, xs[i]);
+        wave_in_order();
+        fetch(b + 4);
+        if (a.dA || a.dbias) {
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const bool there = 4 * h + s < left;
+            for (int j = 0; j < kSteps; ++j) {
+                Frag p[U];
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    const bool ours = there && 32 * u + l < a.dout;
-                    p[w][u][s] = ours ? P[in_p[s] + 32 * u] : 0.0f;
-                    if (a.act) z[w][u][s] = ours ? Z[in_z[s] + 32 * u] : 0.0f;
-                }
+                    p[u] = columns<T>(rows, Block<T, S>::kRow * 16, 32 * u, j, lane);
 #pragma unroll
-                for (int v = 0; v < V; ++v) q[w][v][s] = a.out && there && 32 * v + l < a.din ? Q[in_q[s] + 32 * v] : 0.0f;
+                    for (int i = 0; i < E; ++i) bias[u] += (float)p[u][i];
+                }
+                if (!a.dA) continue;
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const Frag x = columns<T>(rows_x, Block<T, SX>::kRow * 16, 32 * v, j, lane);
+#pragma unroll
+                    for (int u = 0; u < U; ++u) acc[u][v] = mfma(x, p[u], acc[u][v]);
+                }
             }
         }
+        wave_in_order();
+        if (!a.dX) continue;
+        f32x16 out[V] = {};
 #pragma unroll
-        for (int w = 0; w < kAhead; ++w) {
+        for (int s = 0; s < S; ++s) {
+            const Frag p = *reinterpret_cast<const Frag*>(rows + (l * Block<T, S>::kRow + 2 * s + h) * 16);
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (a.act) {
-                    Piece<float> g = __builtin_bit_cast(Piece<float>, p[w][u]);
-                    slopes<float, 4>(g, __builtin_bit_cast(Piece<float>, z[w][u]), a.act);
-                    p[w][u] = __builtin_bit_cast(f32x4, g);
-                }
-                bias[u] += (p[w][u][0] + p[w][u][1]) + (p[w][u][2] + p[w][u][3]);
-#pragma unroll
-                for (int v = 0; v < V; ++v) acc[u][v] = mfma(q[w][v], p[w][u], acc[u][v]);
-            }
+            for (int v = 0; v < V; ++v) out[v] = mfma(*reinterpret_cast<const Frag*>(matrix + ((v * S + s) * 64 + lane) * 16), p, out[v]);
         }
-    }
-    const int64_t slot = group > run ? run_slot(first, lo, run) : -1, count = (int64_t)a.dout * a.din;
-    float* out = slot < 0 ? a.out + e * count : a.parts + slot * count;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
+        // a lane has its row's results, four consecutive ones at a time; they go out in the order of memory
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) sums[wave][v * 16 + r][lane] = acc[u][v][r];
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<float4*>(turned + l * kOut + 32 * v + 8 * g + 4 * h) =
+                    make_float4(out[v][4 * g], out[v][4 * g + 1], out[v][4 * g + 2], out[v][4 * g + 3]);
+        wave_in_order();
+#pragma unroll
+        for (int i = 0; i < SX; ++i) {
+            const int64_t row = first + 32 * (int64_t)b + Q.row[i];
+            if (Q.row[i] >= 32 || row >= end) continue;
+            Piece<T> y;
+#pragma unroll
+            for (int j = 0; j < E; ++j) y.e[j] = (T)turned[Q.row[i] * kOut + Q.from[i] + j];
+            T* to = a.dX + row * a.lddx + Q.from[i];
+            if (a.din >= E) {
+                y.store(to);
+            } else {
+#pragma unroll
+                for (int j = 0; j < E; ++j)
+                    if (j < a.din) to[j] = y.e[j];
+            }
+        }
+        wave_in_order();
+    }
+    if (!a.dA && !a.dbias) return;
+    const int64_t slot = group > run ? run_slot(first, lo, run) : -1, count = (int64_t)a.dout * a.din;
+    float* sums = reinterpret_cast<float*>(narrow_lds);                // of a wavefront: V 1024
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        __syncthreads();                                               // (no one reads what lies there any more)
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sums[(wave * V * 16 + v * 16 + r) * 64 + lane] = acc[u][v][r];
         bias[u] += __shfl_xor(bias[u], 32);
         if (h == 0) bias_sums[wave][32 * u + l] = bias[u];
         __syncthreads();
-        for (int i = threadIdx.x; a.out && i < V * 1024; i += 256) {
-            const int t = i & 63, r = (i >> 6) & 15, c = i >> 6;
+        for (int i = threadIdx.x; a.dA && i < V * 1024; i += 256) {
+            const int t = i & 63, r = (i >> 6) & 15;
             const int m = 32 * u + (t & 31), n = 32 * (i >> 10) + (r & 3) + 8 * (r >> 2) + 4 * (t >> 5);
-            if (m < a.dout && n < a.din) out[(int64_t)m * a.din + n] = (sums[0][c][t] + sums[1][c][t]) + (sums[2][c][t] + sums[3][c][t]);
+            if (m >= a.dout || n >= a.din) continue;
+            const float x = (sums[i] + sums[V * 1024 + i]) + (sums[2 * V * 1024 + i] + sums[3 * V * 1024 + i]);
+            if (slot < 0) a.dA[e * count + (int64_t)m * a.din + n] = (T)x;
+            else a.parts[slot * count + (int64_t)m * a.din + n] = x;
         }
-        __syncthreads();
     }
-    if (dbias && (int)threadIdx.x < a.dout) {
+    if (a.dbias && (int)threadIdx.x < a.dout) {
         const int m = threadIdx.x;
-        float* to = slot < 0 ? dbias + (int64_t)e * a.dout : bias_parts + slot * a.dout;
-        to[m] = (bias_sums[0][m] + bias_sums[1][m]) + (bias_sums[2][m] + bias_sums[3][m]);
+        const float x = (bias_sums[0][m] + bias_sums[1][m]) + (bias_sums[2][m] + bias_sums[3][m]);
+        if (slot < 0) a.dbias[(int64_t)e * a.dout + m] = (T)x;
+        else a.bias_parts[slot * a.dout + m] = x;
     }
 }
 
@@ -308,12 +474,13 @@ static int run_rows(const som_ctx* ctx, int64_t rows, int32_t K, int64_t tiles, 
     return (int)((run + 63) / 64 * 64 < 0x7fffffc0 ? (run + 63) / 64 * 64 : 0x7fffffc0);
 }
 
-// Rows of a run of narrow sums: runs that fill the chip twice, or a group's rows at once where the groups do (but no more than twice its share).
-static int narrow_run(const som_ctx* ctx, int64_t rows, int32_t K)
+// Rows of a run of narrow gradients: 512, fewer where those don't fill the chip (two workgroups a unit) once, more where the runs' sums would
+// become many (200,000 rows 64 -> 64 bf16 on 16 nodes: 391 rows, some more workgroups than fit, 65 us, 512 rows 43; 500,000 rows
+// 64 -> 32 on 100 nodes: 512 rows 63, 1000 rows 74).
+static int narrow_run(const som_ctx* ctx, int64_t rows)
 {
-    const int64_t share = (rows + K - 1) / K, runs = 2 * (int64_t)ctx->units / K, run = runs > 1 ? (share + runs - 1) / runs : 2 * share;
-    const int64_t at_least = run < 256 ? 256 : run;
-    return (int)(at_least < 0x7fffffc0 ? at_least : 0x7fffffc0);
+    const int64_t once = rows / (ctx->units * 7 / 4), many = rows / (ctx->units * 16), run = once < 256 ? 256 : once > 512 ? 512 : once;
+    return (int)(run > many ? run : many);
 }
 
 template <class T, bool AT>
@@ -332,6 +499,30 @@ static int product_narrow_launch(som_ctx* ctx, const ProductArgs<T>& a, const ch
     chunk = chunk < 128 ? 128 : chunk > 1024 ? 1024 : chunk;
     hipLaunchKernelGGL(kern, dim3((unsigned)most_tiles(a.rows, a.K, a.offsets, (int)chunk)), dim3(256), 0, ctx->stream, a, (int)chunk);
     return check_hip(ctx, hipGetLastError(), what);
+}
+
+template <class T, int U, int V>
+static int gradient_narrow_as(som_ctx* ctx, const GradientArgs<T>& a)
+{
+    static bool attr_set_dev[kMaxDevices] = {};
+    bool& attr_set = attr_set_dev[ctx->device];
+    constexpr int lds = Gradient<T, U, V>::LDS;
+    auto kern = gradient_narrow_kernel<T, U, V>;
+    if (!attr_set) {
+        if (int rc = check_hip(ctx, hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds),
+                               "raising the dynamic LDS limit"))
+            return rc;
+        attr_set = true;
+    }
+    hipLaunchKernelGGL(kern, dim3((unsigned)most_runs(a.rows, a.K, a.run)), dim3(256), lds, ctx->stream, a);
+    return check_hip(ctx, hipGetLastError(), "product gradient (narrow) launch");
+}
+
+template <class T>
+static int gradient_narrow_launch(som_ctx* ctx, const GradientArgs<T>& a)
+{
+    if (a.dout <= 32) return a.din <= 32 ? gradient_narrow_as<T, 1, 1>(ctx, a) : gradient_narrow_as<T, 1, 2>(ctx, a);
+    return a.din <= 32 ? gradient_narrow_as<T, 2, 1>(ctx, a) : gradient_narrow_as<T, 2, 2>(ctx, a);
 }
 
 template <class T>

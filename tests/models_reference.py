@@ -16,6 +16,8 @@ TYPES = [torch.float32, torch.bfloat16, torch.float16]
 TILES = [(2000, 16, 136, 2304), (2001, 16, 137, 2303), (3000, 16, 1536, 136), (3001, 16, 1535, 137), (4500, 16, 136, 2560), (4501, 16, 133, 2559),
          (6000, 16, 2048, 136), (6001, 16, 2047, 139), (700, 16, 264, 1032), (701, 16, 263, 1033), (700, 16, 1024, 648), (701, 16, 1023, 649),
          (700, 3, 136, 136), (701, 3, 133, 135), (4100, 1, 512, 4096), (6000, 3, 520, 2304), (6001, 3, 521, 2303), (7000, 6, 1800, 1800)]
+# and narrow ones, whose gradients take every block of results and features in several runs a group
+NARROW = [(5000, 3, 64, 64), (5001, 7, 33, 32), (3000, 2, 17, 40), (70_000, 5, 37, 24), (2000, 1, 3, 5), (4000, 9, 1, 64), (4000, 9, 64, 1), (3001, 4, 50, 47)]
 ACTIVATIONS = ["none", "relu", "silu", "gelu", "gelu_tanh"]
 
 

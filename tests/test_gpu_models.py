@@ -208,7 +208,7 @@ def test_gradient_of_long_groups(som, M, K, Din, Dout, how, act, dtype):
 
 
 @pytest.mark.parametrize("dtype", ref.TYPES)
-@pytest.mark.parametrize("M, K, Din, Dout", ref.TILES)
+@pytest.mark.parametrize("M, K, Din, Dout", ref.TILES + ref.NARROW)
 def test_every_size_of_tile(som, M, K, Din, Dout, dtype):
     """Larger products, against float64 on the GPU: tiles of every size, uneven groups, rows behind the last; twice, to the same bits."""
     gen = torch.Generator().manual_seed(M + Din)

@@ -172,14 +172,18 @@ ROUTES = [  # call, changes, kernels in order
     # one node's last rows apart where they would start another round, and in the tiles where they would not
     ("som_node_product", dict(type=2, M=4099, K=1, offsets=None, Din=4096, ldx=4096, Dout=4096, ldr=4096, ldpre=4096, ldy=4096), ["product_tile", "product_few"]),
     ("som_node_product", dict(type=2, M=4000, K=1, offsets=None, Din=4096, ldx=4096, Dout=4096, ldr=4096, ldpre=4096, ldy=4096), ["product_tile"]),
-    # gradients: slopes and biases in a pass of their own, joins where a group can have more than one run; float32 narrow sums in one
+    # gradients: slopes and biases in a pass of their own, joins where a group can have more than one run; narrow ones at once
     ("som_node_product_grad", dict(type=1, M=300, Din=300, ldx=300, lddx=300), ["slope", "product_tile", "product_tile"]),
     ("som_node_product_grad", dict(type=1, M=9000, Din=300, ldx=300, lddx=300), ["slope", "product_tile", "product_tile", "runs_join", "runs_join"]),
     ("som_node_product_grad", dict(type=1, M=300, Din=300, ldx=300, lddx=300, act=0, dbias=None), ["product_tile", "product_tile"]),
-    ("som_node_product_grad", dict(type=1, M=300, Din=16, dA=None, dbias=None), ["product_narrow"]),
-    ("som_node_product_grad", dict(type=0, M=200, Din=64, ldx=64, lddx=64), ["product_narrow", "sums_narrow"]),
-    ("som_node_product_grad", dict(type=0, M=9000, Din=64, ldx=64, lddx=64), ["product_narrow", "sums_narrow", "runs_join", "runs_join"]),
-    ("som_node_product_grad", dict(type=0, M=200, Din=64, ldx=64, lddx=64, dX=None, dA=None), ["sums_narrow"]),
+    ("som_node_product_grad", dict(type=1, M=300, Din=16, dA=None, dbias=None), ["gradient_narrow"]),
+    ("som_node_product_grad", dict(type=1, M=300, Dout=65, lddy=65, ldpre=65, dA=None, dbias=None), ["product_narrow"]),
+    ("som_node_product_grad", dict(type=1, M=0, dA=None, dbias=None), []),
+    ("som_node_product_grad", dict(type=0, M=200, Din=64, ldx=64, lddx=64), ["gradient_narrow"]),
+    ("som_node_product_grad", dict(type=2, M=9000, Din=64, ldx=64, lddx=64), ["gradient_narrow", "runs_join", "runs_join"]),
+    ("som_node_product_grad", dict(type=0, M=200, Din=64, ldx=64, lddx=64, dX=None, dA=None), ["gradient_narrow"]),
+    ("som_node_product_grad", dict(type=0, M=200, Din=65, ldx=65, lddx=65, act=0, dbias=None), ["product_tile", "product_tile"]),
+    ("som_node_product_grad", dict(type=1, M=200, Dout=65, lddy=65, ldpre=65, act=0, dbias=None), ["product_narrow", "product_tile"]),
 ]
 
 
