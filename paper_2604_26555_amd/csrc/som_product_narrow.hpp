@@ -462,12 +462,13 @@ static int64_t most_tiles(int64_t rows, int32_t K, const int32_t* offsets, int b
 // Runs of `run` rows that the groups can have together.
 static int64_t most_runs(int64_t rows, int32_t K, int run) { return rows / run + K; }
 
-// Rows a run of a sum over rows when a group alone gives `tiles` workgroups: one run a group where the groups fill the chip (longer ones
-// only for a group of four times its share), shorter ones where they do not.
+// Rows a run of a sum over rows when a group alone gives `tiles` workgroups: one run a group where the groups fill the chip (several only for
+// a group of half the rows that a unit takes in all, or four times its share), shorter ones where they do not.
 static int run_rows(const som_ctx* ctx, int64_t rows, int32_t K, int64_t tiles, int least)
 {
     const int64_t share = (rows + K - 1) / K, runs = ctx->units / (K * tiles > ctx->units ? ctx->units : K * tiles);
-    int64_t run = runs > 1 ? (share + runs - 1) / runs : K > 1 ? 4 * share : rows;
+    const int64_t half = K * tiles / (2 * ctx->units);
+    int64_t run = runs > 1 ? (share + runs - 1) / runs : K > 1 ? (half > 4 ? half : 4) * share : rows;
     if (runs <= 1 && run < 2048) run = 2048;
     if (run < least) run = least;
     if (run * 32000 < rows) run = rows / 32000 + 1;             // (a grid's third dimension)

@@ -453,8 +453,20 @@ __global__ void __launch_bounds__(Tile<B>::THREADS) product_tile_kernel(ProductA
         // for 65536 rows, 2048 -> 1536, on 64 uneven nodes, 535 us like this)
         const unsigned ytiles = (a.dout + BM - 1) / BM, each = ytiles * xtiles, share = (each + 7) / 8;
         const unsigned item = each < 16 ? blockIdx.x / each : turn / share, tile = each < 16 ? blockIdx.x % each : xcd * share + turn % share;
-        int which;
-        e = find_group<THREADS>(a.offsets, a.K, a.rows, [run](unsigned n) { return runs_of(n, run); }, item, which);
+        // Groups of more than twice the usual number of rows (kind 0) come first, so that none is the last to start.
+        const unsigned usual = 2u * ((unsigned)a.rows / (unsigned)a.K + 1u);
+        const Item it = find_item<THREADS>(
+            a.offsets, a.K, a.rows,
+            [run, usual](unsigned n) {
+                const unsigned runs = runs_of(n, run);
+                return n > usual ? make_uint2(runs, 0u) : make_uint2(0u, runs);
+            },
+            [item](uint2 total, int& kind) {
+                kind = item < total.x ? 0 : 1;
+                return kind ? item - total.x : item;
+            });
+        e = it.group;
+        const int which = it.which;
         if (e < 0 || tile >= each) return;
         m0 = banded(tile, ytiles, xtiles, x) * BM;
         group_rows(a.offsets, e, a.rows, first, end);
