@@ -204,9 +204,12 @@ int product_grad_typed(som_ctx* ctx, const NodeProductGrad& p)
         a.Q = (const T*)p.A;
         a.out = (T*)p.dX;
         a.ldo = p.lddx;
-        if (int rc = narrow_rows ? product_narrow_launch<T, true>(ctx, a, "product gradient (rows) launch")
-                                 : product_launch<T, kRowsTimesAt>(ctx, a, "product gradient (rows) launch"))
-            return rc;
+        int rc = SOM_OK;
+        if constexpr (sizeof(T) == 2) {
+            if (narrow_rows) rc = product_narrow_launch<T, true>(ctx, a, "product gradient (rows) launch");
+        }
+        if (!narrow_rows) rc = product_launch<T, kRowsTimesAt>(ctx, a, "product gradient (rows) launch");     // (narrow floats: done above)
+        if (rc) return rc;
     }
     a.Q = (const T*)p.X;
     a.ldq = p.ldx;

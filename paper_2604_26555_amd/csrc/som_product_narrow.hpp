@@ -37,7 +37,7 @@ __device__ __forceinline__ typename Fragment<T>::type row_chunk(const T* __restr
     return f;
 }
 
-// Rows of a group times its matrix (AT: dz = P slopes(pre) times the matrix's transpose): a workgroup takes up to `chunk` rows of a group, each of
+// Rows of a group times its matrix (AT: dz = P slopes(pre) times the matrix's transpose, for 65 to 128 16-bit values of dz): a workgroup takes up to `chunk` rows of a group, each of
 // its four wavefronts every fourth block of 32, on its own.  V: blocks of 32 results, S: steps of 32 bytes of the contraction.  Rows come
 // and go in the order of memory, sixteen bytes a lane, through LDS that is the wavefront's own; the next block's are asked for ahead.  (Straight
 // from memory in the matrix pipe's order, 32 bytes of each of 32 rows at a time, 200,000 rows 64 -> 64 bf16 took 41 us, 21 like this.)
@@ -488,12 +488,11 @@ template <class T, bool AT>
 static int product_narrow_launch(som_ctx* ctx, const ProductArgs<T>& a, const char* what)
 {
     const int Nn = AT ? a.din : a.dout, steps = (int)(((AT ? a.dout : a.din) * sizeof(T) + 31) / 32);
-    auto kern = Nn <= 32 ? (steps <= 2   ? product_narrow_kernel<T, AT, 1, 2>
-                            : steps <= 4 ? product_narrow_kernel<T, AT, 1, 4>
-                                         : product_narrow_kernel<T, AT, 1, 8>)
-                         : (steps <= 2   ? product_narrow_kernel<T, AT, 2, 2>
-                            : steps <= 4 ? product_narrow_kernel<T, AT, 2, 4>
-                                         : product_narrow_kernel<T, AT, 2, 8>);
+    auto kern = Nn <= 32 ? product_narrow_kernel<T, AT, 1, 8> : product_narrow_kernel<T, AT, 2, 8>;
+    if constexpr (!AT) {
+        if (steps <= 2) kern = Nn <= 32 ? product_narrow_kernel<T, AT, 1, 2> : product_narrow_kernel<T, AT, 2, 2>;
+        else if (steps <= 4) kern = Nn <= 32 ? product_narrow_kernel<T, AT, 1, 4> : product_narrow_kernel<T, AT, 2, 4>;
+    }
     // Rows of a workgroup: long enough that the matrix and the search for it don't count, short enough to fill the chip four times (500,000
     // rows 64 -> 32 bf16 on 100 nodes: 512 rows 23 us, 1024 rows 29)
     int64_t chunk = (a.rows / (ctx->units * 4) + 127) / 128 * 128;
