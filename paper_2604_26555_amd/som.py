@@ -441,7 +441,7 @@ class Som:
         at, T, k = self._pairs(node, "node", torch.int32)
         if offsets is None:
             offsets = self._empty(int(K) + 1, torch.int32)
-        elif offsets.numel() != int(K) + 1:
+        elif offsets.numel() != int(K) + 1 or offsets.dim() != 1:
             raise ValueError("offsets must have K + 1 entries")
         if order is None:
             order = self._empty(T * k, torch.int32)

@@ -250,3 +250,36 @@ def test_reference_gradients_against_autograd_and_differences(act):
         # the third derivative of a term is below 4 |d . A|^3 |g w|: of some forty terms of size 5 a thousandth of 2^-6 remains
         assert abs(float((got * d).sum() - slope)) <= 2.0 ** -12 * (1 + abs(float(slope)))
     assert off[-1] == int((slot >= 0).sum())
+
+
+class Recorder:
+    """Stands for the library behind the Python wrapper: every call is noted and succeeds."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        return lambda *args: self.calls.append((name, args)) or SOM_OK
+
+
+@pytest.fixture
+def wrapper(monkeypatch):
+    """The Python wrapper on CPU tensors, without a library."""
+    from paper_2604_26555_amd import som as module
+    monkeypatch.setattr(module, "_raw_stream", lambda index: 0)
+    s = module.Som.__new__(module.Som)
+    s.lib, s.device, s._raw, s._h = Recorder(), torch.device("cpu"), 0, None
+    return s
+
+
+def test_group_writes_offsets_only_where_they_lie_side_by_side(wrapper):
+    """K + 1 integers are written from the first entry's address on: a column of a matrix or an expanded number does not hold them."""
+    node, order, slot = (torch.zeros(6, dtype=torch.int32) for _ in range(3))
+    table = torch.zeros(5, 3, dtype=torch.int32)
+    for offsets in (table[:, 1:2], table[:, 1], table[:1, :1].expand(5, 1), table[0, :1].expand(5), table.view(15)[::3], torch.zeros(4, dtype=torch.int32)):
+        with pytest.raises(ValueError):
+            wrapper.som_group(node, 4, offsets=offsets, order=order, slot=slot)
+    assert wrapper.lib.calls == []
+    offsets = torch.zeros(5, dtype=torch.int32)
+    assert wrapper.som_group(node, 4, offsets=offsets, order=order, slot=slot)[0] is offsets
+    assert wrapper.lib.calls[0][1][5] == offsets.data_ptr()
