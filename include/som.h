@@ -324,7 +324,8 @@ int som_epoch_file(som_ctx* ctx, int fd, int64_t offset, int64_t N, int32_t D, i
  * offsets[K] on belong to no node, and what calls would write there is left as it was.  Entries of slot and offsets that point outside
  * M are not followed.  No two pairs share a place (where they do, the place's row is a mixture of what either writes).  Matrices have
  * leading dimensions of their own (>= their width, <= 2^21), any alignment of their elements serves; widths are at most 2^20, T k and M
- * at most 2^31 - 1 (products: M at most 2^31 - 65536), K at most 32768.  Outputs must not overlap inputs or one another.
+ * at most 2^31 - 1 (products: M at most 2^31 - 65536), K at most 32768, places of a row (k of som_dispatch, som_combine and
+ * som_combine_grad) at most 2^20.  Outputs must not overlap inputs or one another.
  */
 enum { SOM_ROWS_FLOAT = 0 /* float32 */, SOM_ROWS_BFLOAT = 1 /* bfloat16 */, SOM_ROWS_HALF = 2 /* float16 */ };
 

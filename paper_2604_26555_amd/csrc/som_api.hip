@@ -370,6 +370,13 @@ static int pairs_check(som_ctx* ctx, int64_t rows, int32_t k)
     return SOM_OK;
 }
 
+// The calls that bring a row to its places or back.
+static int places_check(som_ctx* ctx, int64_t rows, int32_t k)
+{
+    if (int rc = pairs_check(ctx, rows, k)) return rc;
+    return k > kModelPlaces ? fail(ctx, SOM_EINVAL, "more than %d places of a row (k=%d)", kModelPlaces, k) : SOM_OK;
+}
+
 int som_group(som_ctx* ctx, const int32_t* node, int64_t T, int32_t k, int32_t K, int32_t* offsets, int32_t* order, int32_t* slot)
 {
     if (!ctx) return SOM_EINVAL;
@@ -387,7 +394,7 @@ int som_dispatch(som_ctx* ctx, int type, const void* X, int64_t T, int32_t D, in
                  void* Y, int64_t M, int64_t ldy)
 {
     if (!ctx) return SOM_EINVAL;
-    if (int rc = pairs_check(ctx, T, k)) return rc;
+    if (int rc = places_check(ctx, T, k)) return rc;
     if (int rc = rows_checks(ctx, type, M, D, "Y")) return rc;
     if (int rc = matrix_check(ctx, X, T, D, ldx, type, true, "X")) return rc;
     if (int rc = matrix_check(ctx, Y, T ? M : 0, D, ldy, type, true, "Y")) return rc;
@@ -401,7 +408,7 @@ int som_combine(som_ctx* ctx, int type, const void* Y, int64_t M, int32_t D, int
                 const float* weight, void* out, int64_t ldo)
 {
     if (!ctx) return SOM_EINVAL;
-    if (int rc = pairs_check(ctx, T, k)) return rc;
+    if (int rc = places_check(ctx, T, k)) return rc;
     if (int rc = rows_checks(ctx, type, M, D, "Y")) return rc;
     if (int rc = matrix_check(ctx, Y, T ? M : 0, D, ldy, type, true, "Y")) return rc;
     if (int rc = matrix_check(ctx, out, T, D, ldo, type, true, "out")) return rc;
@@ -415,7 +422,7 @@ int som_combine_grad(som_ctx* ctx, int type, const void* dout, int64_t T, int32_
                      const int32_t* slot, int32_t k, const float* weight, void* dY, int64_t lddy, float* dweight)
 {
     if (!ctx) return SOM_EINVAL;
-    if (int rc = pairs_check(ctx, T, k)) return rc;
+    if (int rc = places_check(ctx, T, k)) return rc;
     if (int rc = rows_checks(ctx, type, M, D, "Y")) return rc;
     if (!dY && !dweight) return fail(ctx, SOM_EINVAL, "neither dY nor dweight is asked for");
     if (int rc = matrix_check(ctx, dout, T, D, lddo, type, true, "dout")) return rc;

@@ -214,6 +214,7 @@ int update_static_run(som_ctx* ctx, const double* S, const unsigned long long* n
 constexpr int kGroupNodes = 32768;              // nodes at most: a wavefront's counters of the sort in LDS
 constexpr int kModelWidth = 1 << 20;            // features of a row, and
 constexpr int kModelStride = 1 << 21;           // leading dimension, at most: offsets inside a tile of rows have 32 bits
+constexpr int kModelPlaces = 1 << 20;           // places of a row, at most: one group of lanes walks them, and their number passes the last by a step
 constexpr int kModelRows = 0x7fff0000;          // rows of a product, at most: a row's number may pass the last one by a kernel's step
 int models_workspace(som_ctx* ctx, size_t bytes);
 int group_run(som_ctx* ctx, const int32_t* node, int64_t pairs, int32_t K, int32_t* offsets, int32_t* order, int32_t* slot);

@@ -252,6 +252,16 @@ def test_reference_gradients_against_autograd_and_differences(act):
     assert off[-1] == int((slot >= 0).sum())
 
 
+@pytest.mark.parametrize("name", ["som_dispatch", "som_combine", "som_combine_grad"])
+def test_places_of_a_row_are_bounded(ctx, name):
+    """A row's places are counted in steps of four by one group of lanes, whose count would pass 2^31 - 1 for a single row of as many."""
+    assert call(ctx, name, T=1, k=2 ** 20, M=2 ** 20)[0] == SOM_OK
+    for k in (2 ** 20 + 1, 2 ** 31 - 3, 2 ** 31 - 1):
+        rc, kernels = call(ctx, name, T=1, k=k, M=2 ** 20)
+        assert rc == SOM_EINVAL and kernels == [] and "places of a row" in ctx.error()
+    assert call(ctx, "som_group", T=1, k=2 ** 20 + 1)[0] == SOM_OK              # the sort has pairs only
+
+
 class Recorder:
     """Stands for the library behind the Python wrapper: every call is noted and succeeds."""
 
