@@ -487,3 +487,21 @@ def test_python_refusals(som):
     ]:
         with pytest.raises(error):
             f()
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_left_tails_of_16_bit_activations_to_a_rounding(som, act, dtype):
+    """What is left of an activation far to the left, and its slope there, are as exact as their type and not only small beside z.
+    A result may be off by half a step of its type, and by 2^-13 of itself: the fit of the error function's complement 2^-14.5, the
+    exponents (128 at most in base 2, three roundings of 2^-24) 2^-15.4.  Float32's range ends at 2^-126, where the factors beside the exponential
+    are below 2^8."""
+    X = torch.linspace(-12, -2, 2001)[:, None].to(dtype)
+    A, zero = torch.ones(1, 1, dtype=dtype), torch.zeros_like(X)
+    want, slope = ref.activation(X.double(), act)
+    bound = lambda v: (ref.half_step(dtype) + 2.0 ** -13) * v.abs() + ref.least(dtype) + 2.0 ** -118
+    for rows in (1, 2001):                          # (few rows and many take different kernels)
+        Y = som.som_node_product(X[:rows].cuda(), A.cuda(), activation=act)
+        ref.check(Y, want[:rows], bound(want[:rows]), "Y")
+    dX, _, _ = som.som_node_product_grad(torch.ones_like(X).cuda(), X.cuda(), A.cuda(), pre=X.cuda(), activation=act)
+    ref.check(dX, slope, bound(slope), "dX")
