@@ -223,23 +223,26 @@ __device__ __forceinline__ typename Fragment<T>::type columns(const char* rows, 
     return f.v;
 }
 
-// Chunks of 32 rows of `values` values in the order of memory, chunk number lane + 64 i: what a lane brings.
-template <class T, int S>
+// Chunks of 32 rows of `values` values in the order of memory, chunk number lane + 64 i: what a lane brings.  COLUMN: as if a row had 1, 2, 4 or 8
+// of them, so that a lane's chunks all lie in the same columns; the lanes of chunks that a row does not have bring nothing.
+template <class T, int S, bool COLUMN = false>
 struct Block {
     static constexpr int E = 16 / sizeof(T), kRow = 2 * S + 1;       // LDS rows in chunks, an odd number of them
     typedef typename Fragment<T>::type Frag;
     typedef Frag Any __attribute__((aligned(sizeof(T))));
-    int values, row[S], from[S];
+    int values, chunks, row[S], from[S];
     bool again[S];                                   // a row's last chunk where it is not whole: the row's last sixteen bytes
     __device__ __forceinline__ void init(int n, int lane)
     {
         values = n;
-        const int chunks = (n + E - 1) / E;
+        chunks = (n + E - 1) / E;
+        if (COLUMN) chunks = chunks <= 2 ? chunks : chunks <= 4 ? 4 : 8;
 #pragma unroll
         for (int i = 0; i < S; ++i) {
             const int c = lane + 64 * i;
             row[i] = c / chunks;
             const int at = (c - row[i] * chunks) * E;
+            if (COLUMN && at >= n) row[i] = 32;
             again[i] = n >= E && at + E > n;
             from[i] = again[i] ? n - E : at;
         }
@@ -303,6 +306,7 @@ __global__ void __launch_bounds__(256) gradient_narrow_kernel(GradientArgs<T> a)
     typedef Gradient<T, U, V> G;
     typedef typename Fragment<T>::type Frag;
     constexpr int E = 16 / sizeof(T), S = G::S, SX = G::SX, kOut = G::kOut, kSteps = sizeof(T);     // (32 rows, eight floats or sixteen 16-bit values a step)
+    constexpr bool kExact = sizeof(T) == 2;          // biases add up what dz was before it was rounded: a lane's chunks lie in the same columns
     static_assert(G::LDS >= 4 * V * 4096);
     extern __shared__ __align__(16) char narrow_lds[];
     __shared__ float bias_sums[4][U * 32];
@@ -317,7 +321,7 @@ __global__ void __launch_bounds__(256) gradient_narrow_kernel(GradientArgs<T> a)
     end = end - first > run ? first + run : end;
     char *rows = narrow_lds + wave * G::kWave, *rows_x = rows + G::kRows;
     float* turned = reinterpret_cast<float*>(rows_x);
-    Block<T, S> P;
+    Block<T, S, kExact> P;
     Block<T, SX> Q;
     P.init(a.dout, lane);
     Q.init(a.din, lane);
@@ -351,15 +355,22 @@ __global__ void __launch_bounds__(256) gradient_narrow_kernel(GradientArgs<T> a)
     for (int i = lane; i < G::kRows / 16; i += 64) reinterpret_cast<v4i*>(rows)[i] = v4i{};
     __syncthreads();
     f32x16 acc[U][V] = {};
-    float bias[U] = {};
+    float bias[U] = {}, exact[E] = {};
     for (int b = wave; first + 32 * b < end; b += 4) {
 #pragma unroll
         for (int i = 0; i < S; ++i) {
             Frag x = next[i];
             if (a.act) {
-                Piece<T> g = __builtin_bit_cast(Piece<T>, x);
-                slopes<T, E>(g, __builtin_bit_cast(Piece<T>, zs[i]), a.act);
-                x = __builtin_bit_cast(Frag, g);
+                float dz[E];
+                slopes<T, E>(dz, __builtin_bit_cast(Piece<T>, x), __builtin_bit_cast(Piece<T>, zs[i]), a.act);
+#pragma unroll
+                for (int j = 0; j < E; ++j) {
+                    x[j] = (T)dz[j];
+                    if (kExact) exact[j] += dz[j];
+                }
+            } else if (kExact) {
+#pragma unroll
+                for (int j = 0; j < E; ++j) exact[j] += (float)x[j];
             }
             P.store(i, rows, x);
         }
@@ -368,13 +379,14 @@ __global__ void __launch_bounds__(256) gradient_narrow_kernel(GradientArgs<T> a)
             for (int i = 0; i < SX; ++i) Q.store(i, rows_x, xs[i]);
         wave_in_order();
         fetch(b + 4);
-        if (a.dA || a.dbias) {
+        if (a.dA || (a.dbias && !kExact)) {
 #pragma unroll
             for (int j = 0; j < kSteps; ++j) {
                 Frag p[U];
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     p[u] = columns<T>(rows, Block<T, S>::kRow * 16, 32 * u, j, lane);
+                    if (kExact) continue;
 #pragma unroll
                     for (int i = 0; i < E; ++i) bias[u] += (float)p[u][i];
                 }
@@ -425,6 +437,16 @@ __global__ void __launch_bounds__(256) gradient_narrow_kernel(GradientArgs<T> a)
     if (!a.dA && !a.dbias) return;
     const int64_t slot = group > run ? run_slot(first, lo, run) : -1, count = (int64_t)a.dout * a.din;
     float* sums = reinterpret_cast<float*>(narrow_lds);                // of a wavefront: V 1024
+    if (kExact) {
+        // the lanes of a chunk's columns add theirs up; a column of two chunks takes the one that it begins or goes on in
+#pragma unroll
+        for (int j = 0; j < E; ++j)
+            for (int o = P.chunks; o < 64; o <<= 1) exact[j] += __shfl_xor(exact[j], o);
+        if (lane < P.chunks && P.row[0] == 0)
+#pragma unroll
+            for (int j = 0; j < E; ++j)
+                if (P.from[0] + j >= lane * E && P.from[0] + j < a.dout) bias_sums[wave][P.from[0] + j] = exact[j];
+    }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         __syncthreads();                                               // (no one reads what lies there any more)
@@ -433,7 +455,7 @@ __global__ void __launch_bounds__(256) gradient_narrow_kernel(GradientArgs<T> a)
 #pragma unroll
             for (int r = 0; r < 16; ++r) sums[(wave * V * 16 + v * 16 + r) * 64 + lane] = acc[u][v][r];
         bias[u] += __shfl_xor(bias[u], 32);
-        if (h == 0) bias_sums[wave][32 * u + l] = bias[u];
+        if (!kExact && h == 0) bias_sums[wave][32 * u + l] = bias[u];
         __syncthreads();
         for (int i = threadIdx.x; a.dA && i < V * 1024; i += 256) {
             const int t = i & 63, r = (i >> 6) & 15;

@@ -698,14 +698,14 @@ __global__ void __launch_bounds__(Tile<B>::THREADS) product_tile_kernel(ProductA
     }
 }
 
-// g *= act'(z)
+// dz = g act'(z) in float32
 template <class T, int N>
-__device__ __forceinline__ void slopes(Piece<T, N>& g, const Piece<T, N>& z, int act)
+__device__ __forceinline__ void slopes(float (&dz)[N], const Piece<T, N>& g, const Piece<T, N>& z, int act)
 {
     typedef Math<sizeof(T) == 4> M;
     auto all = [&](int which) {
 #pragma unroll
-        for (int j = 0; j < N; ++j) g.e[j] = (T)((float)g.e[j] * M::slope((float)z.e[j], which));
+        for (int j = 0; j < N; ++j) dz[j] = (float)g.e[j] * M::slope((float)z.e[j], which);
     };
     if (act == SOM_ACT_SILU) all(SOM_ACT_SILU);
     else if (act == SOM_ACT_GELU) all(SOM_ACT_GELU);
@@ -713,8 +713,18 @@ __device__ __forceinline__ void slopes(Piece<T, N>& g, const Piece<T, N>& z, int
     else all(SOM_ACT_RELU);
 }
 
-// dz = dy act'(z), dense (where there is an activation: dz not null), and its column sums over a run of a group's rows (dbias not null):
-// LANES lanes of N columns share a row.
+// g *= act'(z), rounded to the matrix pipe's operand
+template <class T, int N>
+__device__ __forceinline__ void slopes(Piece<T, N>& g, const Piece<T, N>& z, int act)
+{
+    float dz[N];
+    slopes<T, N>(dz, g, z, act);
+#pragma unroll
+    for (int j = 0; j < N; ++j) g.e[j] = (T)dz[j];
+}
+
+// dz = dy act'(z), dense (where there is an activation: dz not null), and its column sums over a run of a group's rows (dbias not null),
+// of the values before they are rounded: LANES lanes of N columns share a row.
 template <class T, int N, int LANES>
 __global__ void __launch_bounds__(256) slope_kernel(const T* __restrict__ dY, int64_t lddy, const T* __restrict__ pre, int64_t ldpre,
                                                     const int32_t* __restrict__ offsets, int K, int rows, int32_t dout, int act, T* __restrict__ dz,
@@ -746,12 +756,19 @@ __global__ void __launch_bounds__(256) slope_kernel(const T* __restrict__ dY, in
             for (int u = 0; u < 4; ++u) {
                 const int r = r0 + u * kRows;
                 if (r >= end) continue;
+                float x[N];
                 if (dz) {
-                    slopes<T, N>(g[u], z[u], act);
-                    g[u].store(dz + (int64_t)r * dout + at);
+                    slopes<T, N>(x, g[u], z[u], act);
+                    Piece<T, N> d;
+#pragma unroll
+                    for (int j = 0; j < N; ++j) d.e[j] = (T)x[j];
+                    d.store(dz + (int64_t)r * dout + at);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < N; ++j) x[j] = (float)g[u].e[j];
                 }
 #pragma unroll
-                for (int j = 0; j < N; ++j) s[j] += (float)g[u].e[j];
+                for (int j = 0; j < N; ++j) s[j] += x[j];
             }
         }
     }

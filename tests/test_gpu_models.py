@@ -505,3 +505,22 @@ def test_left_tails_of_16_bit_activations_to_a_rounding(som, act, dtype):
         ref.check(Y, want[:rows], bound(want[:rows]), "Y")
     dX, _, _ = som.som_node_product_grad(torch.ones_like(X).cuda(), X.cuda(), A.cuda(), pre=X.cuda(), activation=act)
     ref.check(dX, slope, bound(slope), "dX")
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("Din, Dout", [(24, 24), (40, 30), (20, 61), (64, 64), (3, 5), (48, 100), (200, 300), (200, 6)])
+def test_bias_gradients_add_up_what_is_not_rounded_yet(som, Din, Dout, dtype, act):
+    """The products take dz in 16 bits; the biases' gradients are sums of float32 values, and so nearer than dz's roundings would leave them."""
+    gen = torch.Generator().manual_seed(Dout)
+    offsets = torch.tensor([0, 100, 100, 190, 260], dtype=torch.int32)
+    X, A, dY, Z = (normal(gen, *s, dtype=dtype) for s in ((260, Din), (4, Dout, Din), (260, Dout), (260, Dout)))
+    dz = dY.double() * ref.activation(Z.double(), act)[1]
+    dev = (dY.cuda(), X.cuda(), A.cuda(), offsets.cuda(), Z.cuda(), act)
+    dbias = som.som_node_product_grad(*dev)[2]
+    for e in range(4):
+        d = dz[int(offsets[e]):int(offsets[e + 1])]
+        # a slope is off by 32 roundings, the sum by one for each of its terms and two for the product and the joined sums
+        want, size = d.sum(0), (1.2 * dY[int(offsets[e]):int(offsets[e + 1])].double().abs()).sum(0)
+        ref.check(dbias[e], want, ref.rounded(want, (d.shape[0] + 34) * (ref.F32 * size + ref.least(torch.float32)), dtype), f"dbias of node {e}")
+    assert torch.equal(som.som_node_product_grad(*dev, dX=False, dA=False)[2], dbias)
