@@ -383,6 +383,13 @@ class Som:
         with torch.cuda.stream(self.stream):
             return torch.empty(shape, dtype=dtype, device=self.device)
 
+    def _zeros(self, shape, dtype):
+        """The same, cleared: for outputs some of whose rows a call may leave as they were."""
+        if _raw_stream(self.device.index) == self._raw:
+            return torch.zeros(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(self.stream):
+            return torch.zeros(shape, dtype=dtype, device=self.device)
+
     def _rows(self, t, name, dtype=None, shape=None):
         """(address, rows, columns, leading dimension) of a matrix of a local model's rows."""
         if dtype is not None and t.dtype != dtype:
@@ -457,14 +464,14 @@ class Som:
         return offsets, order, slot
 
     def som_dispatch(self, X, slot, weight=None, out=None):
-        """Rows to their places: out[slot[t, j]] = weight[t, j] * X[t] (without weights: X[t]).  out: T k rows unless given;
-        rows that are no pair's place are left as they were."""
+        """Rows to their places: out[slot[t, j]] = weight[t, j] * X[t] (without weights: X[t]).  out: T k rows unless given.
+        Rows that are no pair's place are left as they were in a given out (which saves the clearing) and are zeros in a new one."""
         x, T, D, ldx = self._rows(X, "X")
         s, Ts, k = self._pairs(slot, "slot", torch.int32)
         if Ts != T:
             raise ValueError("slot must have one row per row of X")
         if out is None:
-            out = self._empty((T * k, D), X.dtype)
+            out = self._zeros((T * k, D), X.dtype)
         y, M, Dy, ldy = self._rows(out, "out", X.dtype)
         if Dy != D:
             raise ValueError("out must have X's width")
@@ -484,13 +491,14 @@ class Som:
         return out
 
     def som_combine_grad(self, dout, Y, slot, weight=None, dY=None, dweight=None):
-        """Gradient of som_combine: (dY, dweight).  Either is left out, and returned as None, where False is given for it."""
+        """Gradient of som_combine: (dY, dweight).  Either is left out, and returned as None, where False is given for it.
+        Rows that are no pair's place are left as they were in a given dY and are zeros in a new one."""
         y, M, D, ldy = self._rows(Y, "Y")
         s, T, k = self._pairs(slot, "slot", torch.int32)
         g, _, _, lddo = self._rows(dout, "dout", Y.dtype, (T, D))
         dy = lddy = dw = None
         if dY is None:
-            dY = self._empty((M, D), Y.dtype)
+            dY = self._zeros((M, D), Y.dtype)
         if dY is not False:
             dy, _, _, lddy = self._rows(dY, "dY", Y.dtype, (M, D))
         if dweight is None:
@@ -506,7 +514,8 @@ class Som:
     def som_node_product(self, X, A, offsets=None, bias=None, activation="none", residual=None, pre=None, out=None):
         """Every row times its node's matrix: out[s] = activation(A[e] X[s] + bias[e]) + residual[s] for the rows
         offsets[e] <= s < offsets[e + 1] of node e; without offsets A is one matrix for all rows.  pre, if given, receives the values
-        before the activation.  activation: none, relu, silu, gelu or gelu_tanh."""
+        before the activation.  activation: none, relu, silu, gelu or gelu_tanh.  Rows of no node are left as they were in a given out and
+        are zeros in a new one."""
         x, M, Din, ldx = self._rows(X, "X")
         K, Dout, Da, off = self._nodes(X, A, offsets)
         if Da != Din:
@@ -518,7 +527,7 @@ class Som:
         if pre is not None:
             z, _, _, ldz = self._rows(pre, "pre", X.dtype, (M, Dout))
         if out is None:
-            out = self._empty((M, Dout), X.dtype)
+            out = (self._empty if offsets is None else self._zeros)((M, Dout), X.dtype)
         y, _, _, ldy = self._rows(out, "out", X.dtype, (M, Dout))
         rc = self.lib.som_node_product(self._h, _ROWS[X.dtype], x, M, Din, ldx, off, K, A.data_ptr(), Dout, c, _ACTIVATIONS[activation], r, ldr or Dout,
                                        z, ldz or Dout, y, ldy)
@@ -527,7 +536,8 @@ class Som:
 
     def som_node_product_grad(self, dY, X, A, offsets=None, pre=None, activation="none", dX=None, dA=None, dbias=None):
         """Gradient of som_node_product: (dX, dA, dbias); pre as som_node_product filled it, needed where there is an activation.
-        Each is left out, and returned as None, where False is given for it.  The residual's gradient is dY."""
+        Each is left out, and returned as None, where False is given for it.  The residual's gradient is dY.
+        Rows of no node are left as they were in a given dX and are zeros in a new one."""
         x, M, Din, ldx = self._rows(X, "X")
         K, Dout, Da, off = self._nodes(X, A, offsets)
         if Da != Din:
@@ -537,7 +547,7 @@ class Som:
         if pre is not None:
             z, _, _, ldz = self._rows(pre, "pre", X.dtype, (M, Dout))
         if dX is None:
-            dX = self._empty((M, Din), X.dtype)
+            dX = (self._empty if offsets is None else self._zeros)((M, Din), X.dtype)
         if dX is not False:
             dx, _, _, lddx = self._rows(dX, "dX", X.dtype, (M, Din))
         if dA is None:

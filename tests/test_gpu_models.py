@@ -524,3 +524,57 @@ def test_bias_gradients_add_up_what_is_not_rounded_yet(som, Din, Dout, dtype, ac
         want, size = d.sum(0), (1.2 * dY[int(offsets[e]):int(offsets[e + 1])].double().abs()).sum(0)
         ref.check(dbias[e], want, ref.rounded(want, (d.shape[0] + 34) * (ref.F32 * size + ref.least(torch.float32)), dtype), f"dbias of node {e}")
     assert torch.equal(som.som_node_product_grad(*dev, dX=False, dA=False)[2], dbias)
+
+
+def test_new_outputs_hold_zeros_where_nothing_belongs(som):
+    """Rows without a place and rows of no node, in memory that held NaN before."""
+    gen = torch.Generator().manual_seed(2)
+    T, k, K, D, H = 500, 2, 7, 64, 40
+    node = draw_nodes(gen, T, k, K, "holes").cuda()
+    X, A = torch.randn(T, D, device="cuda"), torch.randn(K, H, D, device="cuda")
+    offsets, _, slot = som.som_group(node, K)
+    end = int(offsets[-1])
+    assert 0 < end < T * k
+    calls = [lambda: som.som_dispatch(X, slot), lambda: som.som_node_product(torch.ones(T * k, D, device="cuda"), A, offsets=offsets),
+             lambda: som.som_combine_grad(X, torch.ones(T * k, D, device="cuda"), slot)[0],
+             lambda: som.som_node_product_grad(torch.ones(T * k, H, device="cuda"), torch.ones(T * k, D, device="cuda"), A, offsets=offsets)[0]]
+    for f in calls:
+        for n in (D, H):
+            held = [torch.full((T * k, n), float("nan"), device="cuda") for _ in range(4)]
+            del held
+        out = f()
+        assert out[:end].any(1).all() and not out[end:].any()
+
+
+def test_new_outputs_are_cleared_in_every_replay(som):
+    """Outputs that the wrapper makes inside a captured graph: rows of no node are zeros again in each replay."""
+    from paper_2604_26555_amd import Som
+    gen = torch.Generator().manual_seed(8)
+    T, K, D, H = 400, 5, 48, 24
+    X, A, node = torch.randn(T, D, device="cuda"), torch.randn(K, H, D, device="cuda"), torch.zeros(T, dtype=torch.int32, device="cuda")
+    stream = torch.cuda.Stream()
+    mine = Som(0, stream)
+
+    def step(s):
+        offsets, _, slot = s.som_group(node, K)
+        Xg = s.som_dispatch(X, slot)
+        return offsets, Xg, s.som_node_product(Xg, A, offsets=offsets), s.som_combine_grad(X, Xg, slot)[0]
+
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        step(mine)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        outs = step(mine)
+    for i, how in enumerate(("even", "holes", "none", "holes")):
+        node.copy_(draw_nodes(gen, T, 1, K, how)[:, 0])
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = step(som)
+        torch.cuda.synchronize()
+        for a, b in zip(outs, eager):
+            assert torch.equal(a, b), f"replay {i}"
+        assert not outs[1][int(outs[0][-1]):].any() and not outs[2][int(outs[0][-1]):].any()
+    mine.close()

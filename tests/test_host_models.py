@@ -293,3 +293,18 @@ def test_group_writes_offsets_only_where_they_lie_side_by_side(wrapper):
     offsets = torch.zeros(5, dtype=torch.int32)
     assert wrapper.som_group(node, 4, offsets=offsets, order=order, slot=slot)[0] is offsets
     assert wrapper.lib.calls[0][1][5] == offsets.data_ptr()
+
+
+def test_rows_that_a_call_leaves_are_zeros_in_new_outputs(wrapper):
+    """What is no pair's place, or no node's row, is not written: in a tensor that the wrapper makes it holds zeros, not what was in memory."""
+    slot, offsets = torch.tensor([[0], [-1], [1]], dtype=torch.int32), torch.tensor([0, 1, 2], dtype=torch.int32)
+    X, A, dY = torch.ones(3, 8), torch.ones(2, 4, 8), torch.ones(3, 4)
+    torch.use_deterministic_algorithms(True)                  # (new memory is filled with NaN then)
+    try:
+        assert torch.isnan(torch.empty(3)).all()
+        new = [wrapper.som_dispatch(X, slot), wrapper.som_combine_grad(X, X, slot)[0], wrapper.som_node_product(X, A, offsets=offsets),
+               wrapper.som_node_product_grad(dY, X, A, offsets=offsets)[0]]
+    finally:
+        torch.use_deterministic_algorithms(False)
+    assert [tuple(t.shape) for t in new] == [(3, 8), (3, 8), (3, 4), (3, 8)] and not any(t.any() for t in new)
+    assert [name for name, _ in wrapper.lib.calls] == ["som_dispatch", "som_combine_grad", "som_node_product", "som_node_product_grad"]
