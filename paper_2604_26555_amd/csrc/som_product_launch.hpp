@@ -16,6 +16,8 @@ static bool product_aligned(const ProductArgs<T>& a)
            sixteen(a.Q) && sixteen(a.out) && sixteen(a.bias) && sixteen(a.residual) && sixteen(a.pre);
 }
 
+constexpr int64_t kTilesWide = 1 << 20;        // workgroups in a row of the grid (a multiple of eight: they go round the dies)
+
 template <class T, Form F, int B, bool ALIGNED>
 static int product_tile_launch(som_ctx* ctx, const ProductArgs<T>& a, const char* what)
 {
@@ -31,9 +33,10 @@ static int product_tile_launch(som_ctx* ctx, const ProductArgs<T>& a, const char
     const int64_t xtiles = ((F == kRowsTimesA ? a.dout : a.din) + B - 1) / B, high = F == kOuterSums ? (a.dout + B - 1) / B : 1, each = high * xtiles;
     const int64_t items = F == kOuterSums ? most_runs(a.rows, a.K, a.run) : most_tiles(a.rows, a.K, a.offsets, B);
     const int64_t groups = F != kOuterSums ? ((items * xtiles + 7) / 8 + 2) * 8 : each < 16 ? items * each : (each + 7) / 8 * 8 * items;
-    if (groups * Tile<B>::THREADS >= (int64_t)1 << 32)
-        return fail(ctx, SOM_EINVAL, "%s: more tiles than a launch holds; call with fewer rows or nodes", what);
-    hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(Tile<B>::THREADS), Tile<B>::LDS, ctx->stream, a, (unsigned)xtiles);
+    // (a grid's dimension holds fewer than 2^32 work-items; the workgroups behind the last find no tile)
+    const int64_t wide = groups < kTilesWide ? groups : kTilesWide, rows_of_grid = (groups + wide - 1) / wide;
+    if (groups >= (int64_t)1 << 31) return fail(ctx, SOM_EINVAL, "%s: more than 2^31 tiles; call with fewer rows or nodes", what);
+    hipLaunchKernelGGL(kern, dim3((unsigned)wide, (unsigned)rows_of_grid), dim3(Tile<B>::THREADS), Tile<B>::LDS, ctx->stream, a, (unsigned)xtiles);
     return check_hip(ctx, hipGetLastError(), what);
 }
 

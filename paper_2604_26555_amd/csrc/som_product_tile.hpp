@@ -447,14 +447,14 @@ __global__ void __launch_bounds__(Tile<B>::THREADS) product_tile_kernel(ProductA
     int e, first, end, m0 = 0;
     unsigned x;
     // The chip's eight dies take workgroups in turn; each gets a run of tiles that share operands in its cache.
-    const unsigned xcd = blockIdx.x % 8, turn = blockIdx.x / 8;
+    const unsigned block = blockIdx.x + blockIdx.y * gridDim.x, xcd = block % 8, turn = block / 8;
     float* part = nullptr;
     if (F == kOuterSums) {
         const unsigned run = a.run;
         // Runs differ in length, so every die takes its share of each run's tiles (a run of groups for each die, as below: 726 us
         // for 65536 rows, 2048 -> 1536, on 64 uneven nodes, 535 us like this)
         const unsigned ytiles = (a.dout + BM - 1) / BM, each = ytiles * xtiles, share = (each + 7) / 8;
-        const unsigned item = each < 16 ? blockIdx.x / each : turn / share, tile = each < 16 ? blockIdx.x % each : xcd * share + turn % share;
+        const unsigned item = each < 16 ? block / each : turn / share, tile = each < 16 ? block % each : xcd * share + turn % share;
         // Groups of more than twice the usual number of rows (kind 0) come first, so that none is the last to start.
         const unsigned usual = 2u * ((unsigned)a.rows / (unsigned)a.K + 1u);
         const Item it = find_item<THREADS>(

@@ -578,3 +578,15 @@ def test_new_outputs_are_cleared_in_every_replay(som):
             assert torch.equal(a, b), f"replay {i}"
         assert not outs[1][int(outs[0][-1]):].any() and not outs[2][int(outs[0][-1]):].any()
     mine.close()
+
+
+def test_more_tiles_than_a_row_of_the_grid(som):
+    """134 million rows of one value and their gradient's 65: more than the 2^20 workgroups that a row of the grid holds, 17 GB of results."""
+    M, D, step = 2 ** 27 + 3, 65, 2 ** 22
+    with torch.device("cuda"):
+        dY, A = torch.randn(M, 1, dtype=torch.float16), torch.randn(1, D).half()
+        dX = som.som_node_product_grad(dY, torch.empty(M, D, dtype=torch.float16), A, dA=False, dbias=False)[0]
+        for lo in range(0, M, step):                 # one product a result: exact in float32, rounded once
+            assert torch.equal(dX[lo:lo + step], (dY[lo:lo + step].float() * A.float()).half()), lo
+    del dX, dY
+    torch.cuda.empty_cache()

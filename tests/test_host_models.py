@@ -252,6 +252,30 @@ def test_reference_gradients_against_autograd_and_differences(act):
     assert off[-1] == int((slot >= 0).sum())
 
 
+@pytest.mark.parametrize("Din", [65, 200])
+@pytest.mark.parametrize("type", [0, 1, 2])
+def test_as_many_rows_as_a_product_takes(ctx, type, Din):
+    """2^31 - 65536 rows, with matrices that go through tiles: their launch holds them in rows of 2^20 workgroups, no dimension 2^32 work-items."""
+    M = 2 ** 31 - 65536
+    for name, changes in (("som_node_product", dict(Dout=1, ldy=1, act=0, bias=None, residual=None, pre=None)),
+                          ("som_node_product_grad", dict(Dout=1, lddy=1, act=0, pre=None, dA=None, dbias=None)),
+                          ("som_node_product_grad", dict(Dout=1, lddy=1, act=0, pre=None, dX=None, dbias=None))):
+        if name == "som_node_product" and type > 0 and Din < 129:
+            continue                                 # (a narrow product)
+        for K, offsets in ((1, None), (32768, "p")):
+            rc, kernels = call(ctx, name, type=type, M=M, Din=Din, ldx=Din, lddx=Din, offsets=offsets, K=K, **changes)
+            assert rc == SOM_OK and "product_tile" in kernels[0], (rc, kernels, ctx.error())
+            _, x, y, z, threads, lds = ctx.launches[0]
+            assert x * threads < 2 ** 32 and y < 65536 and z == 1 and (y == 1 or x % 8 == 0)
+            if changes.get("dX", "p"):
+                rows, width = lds // 512, Din if name.endswith("grad") else 1
+                assert x * y >= (-(-M // rows) + (K if K > 1 else 0)) * -(-width // rows)
+    # the rows of the GPU test that goes beyond one row of the grid
+    M = 2 ** 27 + 3
+    call(ctx, "som_node_product_grad", type=2, M=M, K=1, offsets=None, Din=65, ldx=65, lddx=65, Dout=1, lddy=1, act=0, pre=None, dA=None, dbias=None)
+    assert ctx.launches[0][2] > 1
+
+
 @pytest.mark.parametrize("name", ["som_dispatch", "som_combine", "som_combine_grad"])
 def test_places_of_a_row_are_bounded(ctx, name):
     """A row's places are counted in steps of four by one group of lanes, whose count would pass 2^31 - 1 for a single row of as many."""
