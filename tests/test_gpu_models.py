@@ -590,3 +590,18 @@ def test_more_tiles_than_a_row_of_the_grid(som):
             assert torch.equal(dX[lo:lo + step], (dY[lo:lo + step].float() * A.float()).half()), lo
     del dX, dY
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", ref.TYPES)
+@pytest.mark.parametrize("M, K, Din, Dout, how", [(200, 40, 600, 70, "one"), (95, 10, 512, 33, "skew"), (300, 64, 1029, 48, "skew"), (64, 7, 300, 130, "one"), (77, 1, 520, 40, "one")])
+def test_few_rows_on_uneven_nodes(som, M, K, Din, Dout, how, dtype):
+    """Products whose mean number of rows a node is small, with most rows on one node: several workgroups share a node's rows."""
+    gen = torch.Generator().manual_seed(M)
+    offsets = cut(gen, M, K, how)
+    X, A, c = normal(gen, M, Din, dtype=dtype), normal(gen, K, Dout, Din, dtype=dtype, scale=Din ** -0.5), normal(gen, K, Dout, dtype=dtype)
+    R, before = normal(gen, M, Dout, dtype=dtype), normal(gen, M, Dout, dtype=dtype)
+    out, z = padded(before, 3, 1), padded(before, 1, 0)
+    som.som_node_product(padded(X, 1, 1), A.cuda(), offsets=offsets.cuda(), bias=c.cuda(), activation="silu", residual=padded(R, 2, 1), pre=z, out=out)
+    want, bound, wz, bz = ref.product(X, A, offsets, c, "silu", R, before, before)
+    ref.check(out, want, bound, "Y")
+    ref.check(z, wz, bz, "pre")

@@ -276,6 +276,24 @@ def test_as_many_rows_as_a_product_takes(ctx, type, Din):
     assert ctx.launches[0][2] > 1
 
 
+@pytest.mark.parametrize("M, K, Din, Dout", [(640, 64, 2048, 1024), (10_000, 1000, 2048, 1024), (37, 5, 600, 70), (64, 1, 512, 256), (33, 1, 512, 256)])
+def test_few_rows_have_a_workgroup_for_every_sixteen(ctx, M, K, Din, Dout):
+    """However the rows of few-row products lie on the nodes, all on one among them, each sixteen of a node have workgroups of their own
+    (one node's rows go sixteen, 32 or 64 to one)."""
+    rc, kernels = call(ctx, "som_node_product", type=1, M=M, K=K, offsets="p" if K > 1 else None, Din=Din, ldx=Din, Dout=Dout, ldr=Dout, ldpre=Dout, ldy=Dout)
+    assert rc == SOM_OK and len(kernels) == 1 and "product_few" in kernels[0]
+    across = -(-Dout // 16)
+    if K == 1:
+        assert ctx.launches[0][1] == across
+        return
+    gen = torch.Generator().manual_seed(M)
+    even, one = torch.full((K,), M // K), torch.zeros(K, dtype=torch.long)
+    even[:M % K] += 1
+    one[K // 2] = M
+    for counts in (even, one, torch.bincount((torch.rand(M, generator=gen) ** 6 * K).long(), minlength=K)):
+        assert ctx.launches[0][1] >= int(((counts + 15) // 16).sum()) * across
+
+
 @pytest.mark.parametrize("name", ["som_dispatch", "som_combine", "som_combine_grad"])
 def test_places_of_a_row_are_bounded(ctx, name):
     """A row's places are counted in steps of four by one group of lanes, whose count would pass 2^31 - 1 for a single row of as many."""
