@@ -41,10 +41,12 @@ static int product_tile_launch(som_ctx* ctx, const ProductArgs<T>& a, const char
 }
 
 // Which tiles a call takes: the estimated time of each size in microseconds, from timed steps of 128 bytes of the contraction.
-//   A workgroup alone on its unit takes 1.1, 0.65 and 0.47 us a step (16-bit; 256, 128 and 64 rows), as many as fit 1.6, 1.35 (two) and 1.3 (five);
-//   float32 goes by its products alone: 7.3, 2.05 and 0.55 us each.  Beside its steps a tile takes some 9, 6 and 4 us.  Small tiles fill the
-//   chip where there are few and waste less of narrow matrices, large ones read less: 65536 rows 2048 -> 1536 on 64 nodes 540, 633 and
-//   954 us, 256 rows 4096 -> 4096 on one 80, 46 and 35, 250,013 rows 37 -> 24 in float32 on 437 nodes 148, 98 and 55.
+//   A workgroup alone on its unit takes 1.1, 0.65 and 0.47 us a step (16-bit; 256, 128 and 64 rows), as many as fit (Tile<B>::MOST) 1.6, 1.35
+//   (two) and 1.0 (four; 0.74 where the caches hold all operands); float32 goes by its products alone: 7.3 and 2.05 us each, and for 64
+//   rows 0.55 for one and 0.49 each for four.  Beside its steps a tile takes some 9, 6 and 4 us (float32 5).  Small tiles fill the chip
+//   where there are few and waste less of narrow matrices, large ones read less: 65536 rows 2048 -> 1536 on 64 nodes 540, 633 and 954 us,
+//   256 rows 4096 -> 4096 on one 80, 46 and 35, 250,013 rows 37 -> 24 in float32 on 437 nodes 148, 98 and 55.  Of 2447 products and gradients
+//   drawn between 64 and 4096 wide, the size that this picks takes 1.7 % longer than the best one on average, and 108 take over 15 % longer.
 template <class T, Form F>
 static double tile_time(const som_ctx* ctx, const ProductArgs<T>& a, int B)
 {
@@ -53,10 +55,11 @@ static double tile_time(const som_ctx* ctx, const ProductArgs<T>& a, int B)
     const double tall = a.offsets ? rows / B + 0.5 * groups : (a.rows + B - 1) / B;
     const double tiles = across * (F == kOuterSums ? runs * ((a.dout + B - 1) / B) : tall > groups ? tall : groups);
     const double depth = F == kRowsTimesA ? a.din : F == kRowsTimesAt ? a.dout : rows / runs;
-    const double steps = 1.0 + depth * sizeof(T) / 128.0, more = B == 256 ? 9.0 : B == 128 ? 6.0 : 4.0, most = B == 256 ? 1.0 : B == 128 ? 2.0 : 5.0;
+    const double steps = 1.0 + depth * sizeof(T) / 128.0, more = B == 256 ? 9.0 : B == 128 ? 6.0 : sizeof(T) == 4 ? 5.0 : 4.0;
+    const double most = B == 256 ? Tile<256>::MOST : B == 128 ? Tile<128>::MOST : Tile<64>::MOST;
     auto step = [&](double o) {                         // o workgroups on a unit
-        if (sizeof(T) == 4) return B == 256 ? 7.3 : B == 128 ? 2.05 * o : 0.55 * o;
-        return B == 256 ? 1.1 + 0.5 * o * o : B == 128 ? 0.65 + 0.7 * (o - 1.0) : 0.47 + 0.05 * (o - 1.0) * (o - 1.0);
+        if (sizeof(T) == 4) return B == 256 ? 7.3 : B == 128 ? 2.05 * o : 0.08 + 0.47 * o;
+        return B == 256 ? 1.1 + 0.5 * o * o : B == 128 ? 0.65 + 0.7 * (o - 1.0) : 0.47 + 0.06 * (o - 1.0) * (o - 1.0);
     };
     const double rounds = tiles / (ctx->units * most), whole = (double)(int64_t)rounds, rest = (rounds - whole) * most;
     return whole * (steps * step(most) + more) + (rest > 0.0 ? steps * step(B == 256 ? rest : rest < 1.0 ? 1.0 : rest) + more : 0.0);

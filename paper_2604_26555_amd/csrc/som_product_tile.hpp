@@ -424,10 +424,13 @@ __device__ __forceinline__ unsigned banded(unsigned tile, unsigned rows, unsigne
     return rest / mine;
 }
 
-// Square tiles of B rows and columns in wavefronts of WM x WN.  256: eight wavefronts, one workgroup a unit; 128 and 64: four, two and five of them.
+// Square tiles of B rows and columns in wavefronts of WM x WN: eight wavefronts for 256, four for 128 and 64.  MOST: workgroups that a unit's 160 KB of
+// LDS hold, one, two and four of them (the search's sums in front of the stages take 1 KB, as the stages begin at a multiple of it).
 template <int B>
 struct Tile {
-    static constexpr int WM = B == 256 ? 128 : B / 2, WN = B == 256 ? 64 : B / 2, WAVES = (B / WM) * (B / WN), THREADS = 64 * WAVES, LDS = 2 * 2 * B * 128;
+    static constexpr int UNIT_LDS = 160 * 1024, SEARCH_LDS = 1024;
+    static constexpr int WM = B == 256 ? 128 : B / 2, WN = B == 256 ? 64 : B / 2, WAVES = (B / WM) * (B / WN), THREADS = 64 * WAVES, LDS = 2 * 2 * B * 128,
+                         MOST = UNIT_LDS / (LDS + SEARCH_LDS);
 };
 
 template <class T, Form F, int B, bool ALIGNED>
@@ -440,6 +443,7 @@ __global__ void __launch_bounds__(Tile<B>::THREADS) product_tile_kernel(ProductA
     constexpr int kStage = OpP::kBytes + OpQ::kBytes, BK = OpP::BK;
     extern __shared__ __align__(1024) char tile_lds[];
     typedef typename Fragment<T>::type Frag;
+    static_assert(Tile<B>::MOST >= 1 && sizeof(uint2) * WAVES + 2 * sizeof(int) <= Tile<B>::SEARCH_LDS);
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN) * WN;
