@@ -178,7 +178,7 @@ int product_grad_typed(som_ctx* ctx, const NodeProductGrad& p)
     int lanes, columns;
     auto slopes = slope_kernel_for<T>(p.dout, lanes, columns);
     const int64_t blocks = (p.dout + columns - 1) / columns;
-    a.run = narrow_both ? narrow_run(ctx, p.rows) : run_rows(ctx, p.rows, p.K, (int64_t)((p.dout + 255) / 256) * ((p.din + 255) / 256), 512);
+    a.run = narrow_both ? narrow_run(ctx, p.rows, gradient_narrow_most<T>(p.dout, p.din)) : run_rows(ctx, p.rows, p.K, (int64_t)((p.dout + 255) / 256) * ((p.din + 255) / 256), 512);
     const int bias_run = narrow_both ? a.run : 4096 / lanes;               // (else four rows at a time and lane, four times)
     // workspace: dz, the runs' sums of the matrices, those of the biases
     auto pieces = [](size_t bytes) { return (bytes + 255) / 256 * 256; };

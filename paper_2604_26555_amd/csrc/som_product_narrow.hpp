@@ -299,6 +299,8 @@ struct Gradient {
     static constexpr int S = U * sizeof(T), SX = V * sizeof(T), kOut = 32 * V + 4;
     static constexpr int kRows = 32 * Block<T, S>::kRow * 16, kRowsX = 32 * Block<T, SX>::kRow * 16, kTurned = 32 * kOut * 4;
     static constexpr int kWave = kRows + (kRowsX > kTurned ? kRowsX : kTurned), kMatrix = V * S * 1024, LDS = 4 * kWave + kMatrix;
+    static constexpr int STATIC_LDS = 4 * U * 32 * 4 + 64;                 // sums of the biases and of the search
+    static constexpr int MOST = 2 * (LDS + STATIC_LDS) <= 160 * 1024 ? 2 : 1;      // workgroups that a unit holds, as far as runs reckon with them
 };
 template <class T, int U, int V>
 __global__ void __launch_bounds__(256) gradient_narrow_kernel(GradientArgs<T> a)
@@ -307,7 +309,7 @@ __global__ void __launch_bounds__(256) gradient_narrow_kernel(GradientArgs<T> a)
     typedef typename Fragment<T>::type Frag;
     constexpr int E = 16 / sizeof(T), S = G::S, SX = G::SX, kOut = G::kOut, kSteps = sizeof(T);     // (32 rows, eight floats or sixteen 16-bit values a step)
     constexpr bool kExact = sizeof(T) == 2;          // biases add up what dz was before it was rounded: a lane's chunks lie in the same columns
-    static_assert(G::LDS >= 4 * V * 4096);
+    static_assert(G::LDS >= 4 * V * 4096 && sizeof(float) * 4 * U * 32 + 4 * sizeof(uint2) + 2 * sizeof(int) <= G::STATIC_LDS);
     extern __shared__ __align__(16) char narrow_lds[];
     __shared__ float bias_sums[4][U * 32];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, l = lane & 31;
@@ -497,13 +499,15 @@ static int run_rows(const som_ctx* ctx, int64_t rows, int32_t K, int64_t tiles, 
     return (int)((run + 63) / 64 * 64 < 0x7fffffc0 ? (run + 63) / 64 * 64 : 0x7fffffc0);
 }
 
-// Rows of a run of narrow gradients: 512, fewer where those don't fill the chip (two workgroups a unit) once, more where the runs' sums would
-// become many (200,000 rows 64 -> 64 bf16 on 16 nodes: 391 rows, some more workgroups than fit, 65 us, 512 rows 43; 500,000 rows
-// 64 -> 32 on 100 nodes: 512 rows 63, 1000 rows 74).
-static int narrow_run(const som_ctx* ctx, int64_t rows)
+// Rows of a run of narrow gradients, `most` workgroups a unit: 512, or 1024 where a unit holds one, fewer where those don't fill the chip once,
+// more where the runs' sums would become many, and whole rounds of the four wavefronts' blocks of 32 (200,000 rows 64 -> 64 bf16 on 16
+// nodes: 391 rows, some more workgroups than fit, 65 us, 446 rows 45, 512 rows 43; 500,000 rows 64 -> 32 on 100 nodes: 512 rows 63, 1000
+// rows 74; float32 64 -> 64, one a unit: 100,000 rows 76 us with 256, 60 with 512, 200,000 rows 109 with 512, 88 with 896).
+static int narrow_run(const som_ctx* ctx, int64_t rows, int most)
 {
-    const int64_t once = rows / (ctx->units * 7 / 4), many = rows / (ctx->units * 16), run = once < 256 ? 256 : once > 512 ? 512 : once;
-    return (int)(run > many ? run : many);
+    const int64_t once = rows / (ctx->units * most * 15 / 16), many = rows / (ctx->units * 16), longest = 1024 / most;
+    const int64_t run = once < 256 ? 256 : once > longest ? longest : once;
+    return (int)(((run > many ? run : many) + 127) / 128 * 128);
 }
 
 template <class T, bool AT>
@@ -545,6 +549,14 @@ static int gradient_narrow_launch(som_ctx* ctx, const GradientArgs<T>& a)
 {
     if (a.dout <= 32) return a.din <= 32 ? gradient_narrow_as<T, 1, 1>(ctx, a) : gradient_narrow_as<T, 1, 2>(ctx, a);
     return a.din <= 32 ? gradient_narrow_as<T, 2, 1>(ctx, a) : gradient_narrow_as<T, 2, 2>(ctx, a);
+}
+
+// Workgroups of its kernel that a unit holds.
+template <class T>
+static int gradient_narrow_most(int32_t dout, int32_t din)
+{
+    if (dout <= 32) return din <= 32 ? Gradient<T, 1, 1>::MOST : Gradient<T, 1, 2>::MOST;
+    return din <= 32 ? Gradient<T, 2, 1>::MOST : Gradient<T, 2, 2>::MOST;
 }
 
 template <class T>

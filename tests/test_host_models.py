@@ -165,6 +165,16 @@ def test_a_unit_holds_four_workgroups_of_64_rows(ctx, M, Din, Dout):
                     dA=None, dbias=None) == [128]
 
 
+@pytest.mark.parametrize("M", [60_000, 100_000, 130_000, 200_000])
+def test_narrow_float32_gradients_fill_the_chip_once(ctx, M):
+    """64 values both ways in float32: a workgroup's LDS leaves room for one a unit, so as many runs as there are units at most."""
+    rc, _ = call(ctx, "som_node_product_grad", type=0, M=M, K=1, offsets=None, Din=64, ldx=64, lddx=64, Dout=64, lddy=64, ldpre=64)
+    name, x, _, _, _, lds = ctx.launches[0]
+    assert rc == SOM_OK and "gradient_narrow" in name and 160 * 1024 // lds == 1 and 128 < x <= 256
+    rc, _ = call(ctx, "som_node_product_grad", type=1, M=M, K=1, offsets=None, Din=64, ldx=64, lddx=64, Dout=64, lddy=64, ldpre=64)
+    assert rc == SOM_OK and 160 * 1024 // ctx.launches[0][5] >= 2 and 128 < ctx.launches[0][1] <= 512
+
+
 ROUTES = [  # call, changes, kernels in order
     # narrow rows: up to 64 results and 256 bytes of the contraction
     ("som_node_product", dict(M=5000, Din=64, ldx=64, Dout=64, ldr=64, ldpre=64, ldy=64), ["product_narrow"]),
