@@ -605,3 +605,98 @@ def test_few_rows_on_uneven_nodes(som, M, K, Din, Dout, how, dtype):
     want, bound, wz, bz = ref.product(X, A, offsets, c, "silu", R, before, before)
     ref.check(out, want, bound, "Y")
     ref.check(z, wz, bz, "pre")
+
+
+@pytest.mark.parametrize("dtype", ref.TYPES)
+@pytest.mark.parametrize("M, Din, Dout", [(33, 512, 70), (49, 517, 41), (64, 1024, 130), (64, 1031, 33), (40, 300, 17), (57, 640, 16), (17, 600, 50), (32, 513, 24)])
+def test_up_to_64_rows_of_one_node(som, M, Din, Dout, dtype):
+    """Two and four blocks of sixteen rows to a workgroup: partial last blocks, contractions that end inside a step, results that are no multiple
+    of sixteen, all of the epilogue, matrices with leading dimensions of their own."""
+    gen = torch.Generator().manual_seed(M + Din)
+    X, A, c = normal(gen, M, Din, dtype=dtype), normal(gen, Dout, Din, dtype=dtype, scale=Din ** -0.5), normal(gen, Dout, dtype=dtype)
+    R, before = normal(gen, M, Dout, dtype=dtype), normal(gen, M, Dout, dtype=dtype)
+    for act in ("none", "gelu"):
+        out, z = padded(before, 3, 1), padded(before, 1, 3)
+        som.som_node_product(padded(X, 5, 1), A.cuda(), bias=c.cuda(), activation=act, residual=padded(R, 2, 1), pre=z, out=out)
+        want, bound, wz, bz = ref.product(X, A, None, c, act, R, before, before)
+        ref.check(out, want, bound, "Y")
+        ref.check(z, wz, bz, "pre")
+
+
+@pytest.mark.parametrize("M, Din, Dout", [(4136, 1024, 4096), (4160, 2048, 4096), (4115, 1024, 4096)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_last_rows_of_one_node_apart(som, M, Din, Dout, dtype):
+    """A large product whose last rows go through the kernel of few rows: every matrix with a leading dimension of its own, so that the last rows'
+    places are theirs."""
+    with torch.device("cuda"):
+        g = torch.Generator(device="cuda").manual_seed(M)
+        rnd = lambda *s, scale=1.0: (torch.randn(*s, generator=g) * scale).to(dtype)
+        wide = lambda t, extra: torch.cat([t, torch.full((M, extra), float("nan"), dtype=dtype)], 1)[:, :t.shape[1]]
+        X, A, c, R, before = rnd(M, Din), rnd(Dout, Din, scale=Din ** -0.5), rnd(Dout), rnd(M, Dout), rnd(M, Dout)
+        out, z = wide(before, 8), wide(before, 24)
+        som.som_node_product(wide(X, 16), A, bias=c, activation="silu", residual=wide(R, 32), pre=z, out=out)
+        want, bound, wz, bz = ref.product(X, A, None, c, "silu", R, before, before)
+        ref.check(out, want, bound, "Y")
+        ref.check(z, wz, bz, "pre")
+
+
+@pytest.mark.parametrize("dtype", ref.TYPES)
+@pytest.mark.parametrize("Din, Dout", [(24, 16), (200, 136), (37, 70), (136, 3)])
+def test_gradients_with_offsets_outside_the_rows(som, Din, Dout, dtype):
+    """Offsets before the first row and behind the last: the gradients are those of the rows that exist.  Falling ones: nothing outside the
+    matrices' own memory is written."""
+    gen = torch.Generator().manual_seed(Din)
+    M, K = 60, 3
+    X, A, dY, Z = (normal(gen, *s, dtype=dtype) for s in ((M, Din), (K, Dout, Din), (M, Dout), (M, Dout)))
+    before = normal(gen, M, Din, dtype=dtype)
+    for offsets, inside in (([-5, 8, 8, 1000], [0, 8, 8, 60]), ([-100, -7, 60, 2 ** 31 - 1], [0, 0, 60, 60]), ([3, 70, 80, 90], [3, 60, 60, 60])):
+        dX = padded(before, 2, 1)
+        got = som.som_node_product_grad(dY.cuda(), X.cuda(), A.cuda(), offsets=torch.tensor(offsets, dtype=torch.int32).cuda(), pre=Z.cuda(), activation="silu", dX=dX)
+        want = ref.product_grad(dY, X, A, torch.tensor(inside), Z, "silu", before)
+        for g, i, name in zip(got, (0, 2, 4), ("dX", "dA", "dbias")):
+            ref.check(g, want[i], want[i + 1], name)
+    guard = 4096
+
+    def guarded(*shape):
+        n = math.prod(shape)
+        buf = torch.full((n + 2 * guard,), 7.0, dtype=dtype, device="cuda")
+        return buf, buf[guard:guard + n].view(*shape)
+
+    bufs = [guarded(M, Din), guarded(K, Dout, Din), guarded(K, Dout)]
+    for offsets in ([9, 3, 99, 50], [60, 0, 60, 0], [50, 60, 5, 60]):
+        som.som_node_product_grad(dY.cuda(), X.cuda(), A.cuda(), offsets=torch.tensor(offsets, dtype=torch.int32).cuda(), pre=Z.cuda(), activation="silu",
+                                  dX=bufs[0][1], dA=bufs[1][1], dbias=bufs[2][1])
+        for buf, _ in bufs:
+            assert (buf[:guard] == 7).all() and (buf[-guard:] == 7).all()
+
+
+@pytest.mark.parametrize("Din, Dout", [(2048, 1024), (2050, 1022)])
+def test_matrices_behind_two_billion_values(som, Din, Dout):
+    """The last nodes' matrices lie further than 2^31 values from the first one's start: products by few rows and by tiles, gradients."""
+    K = 2 ** 31 // (Din * Dout) + 6
+    with torch.device("cuda"):
+        A = torch.zeros(K, Dout, Din, dtype=torch.bfloat16)
+        A[-2:] = torch.randn(2, Dout, Din) / 45
+        assert (K - 2) * Dout * Din > 2 ** 31
+        for M in (20, 40_000):                          # rows of the last two nodes: five, and the others
+            X, dY = torch.randn(M, Din).bfloat16(), torch.randn(M, Dout).bfloat16()
+            offsets = torch.zeros(K + 1, dtype=torch.int32)
+            offsets[-2], offsets[-1] = 5, M
+            Y = som.som_node_product(X, A, offsets=offsets)
+            cut = (slice(0, 5), slice(5, min(M, 400)))
+            for e, rows in zip((-2, -1), cut):
+                x, a = X[rows].double(), A[e].double()
+                want = x @ a.t().contiguous()
+                ref.check(Y[rows], want, ref.rounded(want, Din * ref.F32 * (x.abs() @ a.abs().t().contiguous()), X.dtype), "Y")
+            dX, dA, _ = som.som_node_product_grad(dY, X, A, offsets=offsets)
+            for e, rows in zip((-2, -1), cut):
+                g, a = dY[rows].double(), A[e].double()
+                want = g @ a
+                ref.check(dX[rows], want, ref.rounded(want, Dout * ref.F32 * (g.abs() @ a.abs()), X.dtype), "dX")
+            g, x = dY[:5].double(), X[:5].double()
+            want = g.t().contiguous() @ x
+            ref.check(dA[-2], want, ref.rounded(want, 5 * ref.F32 * (g.abs().t().contiguous() @ x.abs()), X.dtype), "dA")
+            assert not dA[:-2].any() and dA[-1].any()
+            del dA, dX, Y
+    del A
+    torch.cuda.empty_cache()

@@ -175,6 +175,23 @@ def test_narrow_float32_gradients_fill_the_chip_once(ctx, M):
     assert rc == SOM_OK and 160 * 1024 // ctx.launches[0][5] >= 2 and 128 < ctx.launches[0][1] <= 512
 
 
+@pytest.mark.parametrize("type", [0, 1, 2])
+@pytest.mark.parametrize("M, Din, Dout, blocks", [(33, 512, 70, 4), (49, 517, 41, 4), (64, 1024, 130, 4), (64, 1031, 33, 4), (40, 300, 17, 4), (57, 640, 16, 4),
+                                                  (17, 600, 50, 2), (32, 513, 24, 2)])
+def test_blocks_of_one_nodes_few_rows(ctx, type, M, Din, Dout, blocks):
+    """The shapes of the GPU tests of few rows take kernels of two and four blocks of sixteen rows."""
+    rc, kernels = call(ctx, "som_node_product", type=type, M=M, K=1, offsets=None, Din=Din, ldx=Din, Dout=Dout, ldr=Dout, ldpre=Dout, ldy=Dout)
+    assert rc == SOM_OK and len(kernels) == 1 and "product_few" in kernels[0] and f"Li{blocks}E" in kernels[0].replace(f",{blocks}>", f"Li{blocks}E")
+
+
+@pytest.mark.parametrize("type", [1, 2])
+@pytest.mark.parametrize("M, Din, Dout, blocks", [(4136, 1024, 4096, 4), (4160, 2048, 4096, 4), (4115, 1024, 4096, 2)])
+def test_last_rows_apart_take_blocks(ctx, type, M, Din, Dout, blocks):
+    """The large products of the GPU tests leave their last rows to the kernel of few rows."""
+    rc, kernels = call(ctx, "som_node_product", type=type, M=M, K=1, offsets=None, Din=Din, ldx=Din + 16, Dout=Dout, ldr=Dout + 32, ldpre=Dout + 24, ldy=Dout + 8)
+    assert rc == SOM_OK and len(kernels) == 2 and "product_few" in kernels[1] and f"Li{blocks}E" in kernels[1].replace(f",{blocks}>", f"Li{blocks}E")
+
+
 ROUTES = [  # call, changes, kernels in order
     # narrow rows: up to 64 results and 256 bytes of the contraction
     ("som_node_product", dict(M=5000, Din=64, ldx=64, Dout=64, ldr=64, ldpre=64, ldy=64), ["product_narrow"]),
