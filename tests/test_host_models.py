@@ -184,6 +184,13 @@ def test_blocks_of_one_nodes_few_rows(ctx, type, M, Din, Dout, blocks):
     assert rc == SOM_OK and len(kernels) == 1 and "product_few" in kernels[0] and f"Li{blocks}E" in kernels[0].replace(f",{blocks}>", f"Li{blocks}E")
 
 
+@pytest.mark.parametrize("K, Din, Dout, few", [(62, 264, 768, True), (63, 264, 768, False), (200, 1240, 512, False), (200, 1256, 512, True), (40, 248, 64, False), (40, 256, 64, True)])
+def test_where_few_rows_have_a_kernel_of_their_own(ctx, K, Din, Dout, few):
+    """Rows of 512 bytes and more; up to 3000 workgroups of sixteen results, or any number of them where the rows have 2500 bytes."""
+    rc, kernels = call(ctx, "som_node_product", type=1, M=4 * K, K=K, Din=Din, ldx=Din, Dout=Dout, ldr=Dout, ldpre=Dout, ldy=Dout)
+    assert rc == SOM_OK and len(kernels) == 1 and ("product_few" if few else "product_tile") in kernels[0], kernels
+
+
 @pytest.mark.parametrize("type", [1, 2])
 @pytest.mark.parametrize("M, Din, Dout, blocks", [(4136, 1024, 4096, 4), (4160, 2048, 4096, 4), (4115, 1024, 4096, 2)])
 def test_last_rows_apart_take_blocks(ctx, type, M, Din, Dout, blocks):
