@@ -326,6 +326,11 @@ int som_epoch_file(som_ctx* ctx, int fd, int64_t offset, int64_t N, int32_t D, i
  * leading dimensions of their own (>= their width, <= 2^21), any alignment of their elements serves; widths are at most 2^20, T k and M
  * at most 2^31 - 1 (products: M at most 2^31 - 65536), K at most 32768, places of a row (k of som_dispatch, som_combine and
  * som_combine_grad) at most 2^20.  Outputs must not overlap inputs or one another.
+ *
+ * Memory that the library allocates for these calls and keeps until som_destroy, the largest of what they asked for: som_group of more
+ * than 16384 pairs (or K above 8207) 4 (K + 1) bytes for each 256 pairs, at most for 1024 parts of them, and 8 (K + 1); som_node_product_grad
+ * M Dout values of dz where there is an activation and not both widths are at most 64, and where a node's rows may be summed in several runs
+ * two float32 matrices (and biases) a run.  SOM_ENOMEM where it finds none.
  */
 enum { SOM_ROWS_FLOAT = 0 /* float32 */, SOM_ROWS_BFLOAT = 1 /* bfloat16 */, SOM_ROWS_HALF = 2 /* float16 */ };
 
@@ -383,7 +388,9 @@ int som_node_product(som_ctx* ctx, int type, const void* X, int64_t M, int32_t D
 
 /*
  * Its gradient: dz_s = dY_s act'(z_s);  dX_s = A_e^T dz_s,  dA_e = sum_s dz_s x_s^T,  dbias_e = sum_s dz_s  (a node without rows:
- * zeros); the residual's gradient is dY.  dz is rounded to `type` (the matrix pipe's operand) where an activation changes it.
+ * zeros); the residual's gradient is dY.  In the products dz is rounded to `type` (the matrix pipe's operand) where an activation changes
+ * it, which in 16 bits adds its rounding to the results' own (1.4 times their error), and makes a float16 dz infinite from 65520 on and zero
+ * below 2^-25, as a tensor of that type would hold it; a slope is 1.13 at most.  The biases' sums take dz in float32.
  *   dY [device] M x Dout, lddy;  X, offsets, A as above (A is read for dX, X for dA);  pre [device] as som_node_product wrote it,
  *   required unless activation is SOM_ACT_NONE
  *   dX [device] M x Din, lddx, or NULL;  dA [device] K x Dout x Din, dense, or NULL;  dbias [device] K x Dout, dense, or NULL;

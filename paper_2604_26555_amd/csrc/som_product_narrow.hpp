@@ -495,7 +495,6 @@ static int run_rows(const som_ctx* ctx, int64_t rows, int32_t K, int64_t tiles, 
     int64_t run = runs > 1 ? (share + runs - 1) / runs : K > 1 ? (half > 4 ? half : 4) * share : rows;
     if (runs <= 1 && run < 2048) run = 2048;
     if (run < least) run = least;
-    if (run * 32000 < rows) run = rows / 32000 + 1;             // (a grid's third dimension)
     return (int)((run + 63) / 64 * 64 < 0x7fffffc0 ? (run + 63) / 64 * 64 : 0x7fffffc0);
 }
 

@@ -47,7 +47,7 @@ struct ProductArgs {
     int64_t ldo;
     int act;
     // Sums over rows (kOuterSums): a group's rows are taken in runs of `run`, every run's sum by another workgroup; with more than one run
-    // a group, the sums go to `parts` in float32 (runs_slot) and are added up in order afterwards
+    // a group, the sums go to `parts` in float32 (run_slot) and are added up in order afterwards
     int run;
     float* parts;
 };

@@ -376,6 +376,8 @@ class Som:
         return G
 
     # ------------------------------------------------------------------ local models: one matrix per node
+    # (The calls read tensors as they are, also those that require a gradient: results carry no graph of torch's.  The way back is the
+    # calls whose names end in _grad.)
     def _empty(self, shape, dtype):
         """A new tensor that this context's stream may write at once: its memory comes from that stream's pool."""
         if _raw_stream(self.device.index) == self._raw:
@@ -537,7 +539,8 @@ class Som:
     def som_node_product_grad(self, dY, X, A, offsets=None, pre=None, activation="none", dX=None, dA=None, dbias=None):
         """Gradient of som_node_product: (dX, dA, dbias); pre as som_node_product filled it, needed where there is an activation.
         Each is left out, and returned as None, where False is given for it.  The residual's gradient is dY.
-        Rows of no node are left as they were in a given dX and are zeros in a new one."""
+        With an activation and 16-bit rows, dX and dA are products of dz = dY activation'(pre) rounded to that type (float16: infinite
+        from 65520 on); dbias sums it in float32.  Rows of no node are left as they were in a given dX and are zeros in a new one."""
         x, M, Din, ldx = self._rows(X, "X")
         K, Dout, Da, off = self._nodes(X, A, offsets)
         if Da != Din:
