@@ -292,7 +292,7 @@ struct GradientArgs {
 // sums stay in registers until the wavefronts add theirs up in order.  U and V: blocks of 32 results and features.  The matrix lies in LDS as
 // well: in registers it leaves one wavefront a SIMD instead of two (250,013 rows 37 -> 24 in float32 on 437 nodes 109 us, 81 like this).
 // Slopes, rows and sums in passes of their own took 86 us there (floor of the bytes 26), 71 for 200,000 rows 64 -> 64 bf16 on 16 nodes (now
-// 44, floor 22), 88 for 250,000 rows 37 -> 24 bf16 on 437 (now 49, floor 13).  What is left is the matrix pipe's float32 rate on blocks of
+// 44, floor 22), 88 for 250,000 rows 37 -> 24 bf16 on 437 (now 53, floor 13).  What is left is the matrix pipe's float32 rate on blocks of
 // 32 that are half empty, and a run's start and end.
 template <class T, int U, int V>
 struct Gradient {
