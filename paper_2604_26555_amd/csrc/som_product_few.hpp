@@ -83,9 +83,8 @@ __global__ void __launch_bounds__(512) product_few_kernel(ProductArgs<T> a, unsi
 
 // Where the matrices' bytes decide: up to 64 rows of one node (4096 -> 4096 bf16: 1 row 31 us by tiles of 64 and 11 like this, 64 rows 34 and 23),
 // and up to 10 of several on average, of 512 bytes and more (2048 -> 1536 bf16 on 64 nodes: 4 rows each 96 and 88 us, but 32 each 101 and
-// 203, as every sixteen results bring all rows).  A workgroup reads sixteen rows of a matrix: where that is little and there are many of
-// them, their starts count.  Of 226 products drawn with up to 10 rows a node,
-// time against that of tiles, geometric means:
+// 203, as every sixteen results bring all rows).  A workgroup reads sixteen rows of a matrix: where that is little and there are many
+// workgroups, their starts count.  Of 226 products drawn with up to 10 rows a node, time against that of tiles, geometric means:
 //   rows of      512 to 1024 bytes: 0.95 up to 2048 workgroups, 1.33 from there to 4096, 1.36 beyond;   1024 to 2200: 0.87, 0.83, 1.07
 //               2200 to 4096: 0.66, 0.84, 0.98;   4096 to 20,000: 0.42, 0.85, 0.93
 // so 3000 workgroups, or any number of them for rows of 2500 bytes: 1.5 % above the better of the two on average (2048 and 4096: 2.2 %; 6000

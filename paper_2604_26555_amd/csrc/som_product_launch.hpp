@@ -96,9 +96,9 @@ int product_typed(som_ctx* ctx, const NodeProduct& p)
     a.dout = p.dout;
     a.bias = (const T*)p.bias;
     a.residual = (const T*)p.residual;
-    a.ldr = p.ldr;
+    a.ldr = p.residual ? p.ldr : 0;
     a.pre = (T*)p.pre;
-    a.ldpre = p.ldpre;
+    a.ldpre = p.pre ? p.ldpre : 0;
     a.out = (T*)p.out;
     a.ldo = p.ldo;
     a.act = p.act;
@@ -179,7 +179,8 @@ int product_grad_typed(som_ctx* ctx, const NodeProductGrad& p)
     int lanes, columns;
     auto slopes = slope_kernel_for<T>(p.dout, lanes, columns);
     const int64_t blocks = (p.dout + columns - 1) / columns;
-    a.run = narrow_both ? narrow_run(ctx, p.rows, gradient_narrow_most<T>(p.dout, p.din)) : run_rows(ctx, p.rows, p.K, (int64_t)((p.dout + 255) / 256) * ((p.din + 255) / 256), 512);
+    a.run = narrow_both ? narrow_run(ctx, p.rows, gradient_narrow_most<T>(p.dout, p.din))
+                        : run_rows(ctx, p.rows, p.K, (int64_t)((p.dout + 255) / 256) * ((p.din + 255) / 256), 512);
     const int bias_run = narrow_both ? a.run : 4096 / lanes;               // (else four rows at a time and lane, four times)
     // workspace: dz, the runs' sums of the matrices, those of the biases
     auto pieces = [](size_t bytes) { return (bytes + 255) / 256 * 256; };
@@ -205,8 +206,10 @@ int product_grad_typed(som_ctx* ctx, const NodeProductGrad& p)
     a.P = stored ? dz : (const T*)p.dY;
     a.ldp = stored ? p.dout : p.lddy;
     a.act = stored ? SOM_ACT_NONE : p.act;
-    a.pre = (T*)p.pre;
-    a.ldpre = p.ldpre;
+    if (a.act != SOM_ACT_NONE) {                        // (else no kernel below reads pre, and how it lies is of no account)
+        a.pre = (T*)p.pre;
+        a.ldpre = p.ldpre;
+    }
     if (!narrow_both && p.dX && p.rows > 0) {
         a.Q = (const T*)p.A;
         a.out = (T*)p.dX;

@@ -184,6 +184,18 @@ def test_blocks_of_one_nodes_few_rows(ctx, type, M, Din, Dout, blocks):
     assert rc == SOM_OK and len(kernels) == 1 and "product_few" in kernels[0] and f"Li{blocks}E" in kernels[0].replace(f",{blocks}>", f"Li{blocks}E")
 
 
+def test_only_what_is_read_decides_how_gradients_are_read(ctx):
+    """The slopes' pass reads the values before the activation; the products of dz that follow do not, and take the direct way to LDS whatever
+    the leading dimension of those values."""
+    for ldpre in (1024, 1025):
+        rc, kernels = call(ctx, "som_node_product_grad", type=2, M=3000, Din=1024, ldx=1024, lddx=1024, Dout=1024, lddy=1024, ldpre=ldpre)
+        assert rc == SOM_OK and [k for k in kernels if "product_tile" in k] and all("Lb1E" in k for k in kernels if "product_tile" in k), kernels
+    rc, kernels = call(ctx, "som_node_product_grad", type=2, M=3000, Din=1024, ldx=1025, lddx=1024, Dout=1024, lddy=1024, ldpre=1024)
+    assert rc == SOM_OK and ["Lb1E" in k for k in kernels if "product_tile" in k] == [True, False], kernels
+    rc, kernels = call(ctx, "som_node_product", type=2, M=3000, Din=1024, ldx=1024, Dout=1024, ldy=1024, residual=None, ldr=1, pre=None, ldpre=3)
+    assert rc == SOM_OK and len(kernels) == 1 and "product_tile" in kernels[0] and "Lb1E" in kernels[0], kernels
+
+
 @pytest.mark.parametrize("K, Din, Dout, few", [(62, 264, 768, True), (63, 264, 768, False), (200, 1240, 512, False), (200, 1256, 512, True), (40, 248, 64, False), (40, 256, 64, True)])
 def test_where_few_rows_have_a_kernel_of_their_own(ctx, K, Din, Dout, few):
     """Rows of 512 bytes and more; up to 3000 workgroups of sixteen results, or any number of them where the rows have 2500 bytes."""
